@@ -393,6 +393,163 @@ prox_status prox_allocate_sparsity(double e, double alpha, double s_ref, double 
 prox_status prox_add_rmsnorm(const void *x, const void *y, int batch, int d_model,
                              prox_dtype dtype, float eps, void *out, hipStream_t stream);
 
+/*
+ * ---- The attention half of a decoder layer --------------------------------
+ *
+ * What stands around the FFN of a decode step whose weights are INT4: the
+ * projections (q, k, v, output) on the same INT4 format, the key/value cache
+ * held in 4 bits, and attention over it.
+ *
+ * Projection on INT4 weights:  y_b[j] = sum_g sigma_{j,g} sum_{i in g} x_b[i]
+ * q_{j,i} + bias[j], fp32 accumulation, rounded once to the dtype.  Quantised
+ * as prox_w4_weights: per output j and group of `group` consecutive inputs a
+ * scale sigma = amax / 7 rounded to fp16, codes q = round-half-even(w / sigma)
+ * clamped to [-7, 7], 0 where sigma is 0.  The blob (device, 256-byte aligned,
+ * prox_linear_w4_bytes() bytes) is opaque.  All fields are inputs.
+ */
+#define PROX_MAX_LINEAR_N (1 << 20)
+#define PROX_MAX_LINEAR_K 65536
+typedef struct {
+    int dtype;     /* prox_dtype of x, bias and y (and of the weights packed from) */
+    int n;         /* outputs, 1 .. PROX_MAX_LINEAR_N */
+    int k;         /* inputs, a multiple of group, at most PROX_MAX_LINEAR_K */
+    int group;     /* 32, 64 or a multiple of 128 */
+    void *blob;
+    size_t bytes;
+} prox_w4_linear;
+
+/* Bytes of the blob for this shape; 0 if unsupported. */
+size_t prox_linear_w4_bytes(int n, int k, int group);
+
+/* Quantise w (device [n][k], q->dtype, 16-byte aligned: nn.Linear's weight)
+ * into q->blob (bit-exact, deterministic). */
+prox_status prox_pack_linear_w4(const void *w, const prox_w4_linear *q, hipStream_t stream);
+
+/* Inverse view, for inspection and tests: codes int8 [n][k] and scales (fp16
+ * bits) [n][k / group], both device pointers. */
+prox_status prox_unpack_linear_w4(const prox_w4_linear *q, int8_t *codes, uint16_t *scales,
+                                  hipStream_t stream);
+
+/* The projection of 1 <= batch <= PROX_MAX_BATCH rows.
+ *   x     device, row b at x + b * ldx elements, 16-byte aligned; ldx >= k, a
+ *         multiple of 8 (ignored for one row)
+ *   bias  device [n] (2-byte aligned), or NULL
+ *   y     device, row b at y + b * ldy, 2-byte aligned; ldy >= n (ignored for one
+ *         row); must not overlap x
+ * One launch, no workspace.  Results do not depend on ldx, ldy or the batch's
+ * other rows' values. */
+prox_status prox_linear_w4(const prox_w4_linear *q, const void *x, int64_t ldx, int batch,
+                           const void *bias, void *y, int64_t ldy, hipStream_t stream);
+
+/*
+ * Key/value cache in 4 bits, in pages.  Every key and value of a kv head is
+ * quantised by itself, per group of `group` consecutive channels: sigma =
+ * min(amax / 7 rounded to fp16, 65504), codes c = round-half-even(x / sigma)
+ * clamped to [-7, 7], 0 where sigma is 0; it stands for sigma c.  A page holds
+ * page_size tokens of every kv head: head_dim + 4 head_dim / group bytes per
+ * token and head, keys and values together.  The blob (device, 256-byte
+ * aligned, prox_kv_bytes() bytes) is opaque and needs no initialisation.
+ */
+typedef struct {
+    int dtype;      /* prox_dtype of keys, values, queries and the output */
+    int kv_heads;   /* 1 .. 256 */
+    int head_dim;   /* 64, 128 or 256 */
+    int group;      /* 32, 64 or 128, at most head_dim */
+    int page_size;  /* tokens, a multiple of 32, at most 32768 */
+    int n_pages;    /* 1 .. 2^24 */
+    void *blob;
+    size_t bytes;
+} prox_kv_cache;
+
+/* Bytes of the blob; 0 if unsupported. */
+size_t prox_kv_bytes(int kv_heads, int head_dim, int group, int page_size, int n_pages);
+
+/*
+ * The sequences of a call and their new tokens.  The rows of q, k, v and of the
+ * outputs are the new tokens, sequence after sequence: those of sequence s are
+ * rows cu_new[s] .. cu_new[s + 1] - 1, or, with cu_new NULL, max_new rows each.
+ * They are the last tokens of the sequence: row i of the m of sequence s stands
+ * at position kv_len[s] - m + i, on page page_table[s][position / page_size].
+ * A row whose position is negative (a padded sequence: kv_len[s] < m) has no
+ * place; rows from cu_new[n_seq] on belong to no sequence and are left as they
+ * are, inputs and outputs alike.  Lengths are read on the device, so a captured
+ * call follows them:
+ *   kv_len     above max_kv counts as max_kv, below 0 as 0
+ *   cu_new     entries outside [0, n_tokens] count as its nearer end, falling
+ *              ones as no rows; rows past the max_new first of a sequence are
+ *              left as they are
+ *   page_table a position whose entry lies outside [0, n_pages) is not stored,
+ *              reads as 0 and is hidden from attention
+ * Two sequences may share pages that a call only reads; pages that a call
+ * appends to must belong to one sequence.
+ */
+typedef struct {
+    int n_seq;                   /* 1 .. 65536 */
+    int max_new;                 /* the most new tokens of a sequence, >= 1 */
+    int n_tokens;                /* rows of q, k, v and the outputs; n_seq * max_new without cu_new */
+    int max_kv;                  /* the longest kv_len, 1 .. max_pages * page_size; 0: max_pages * page_size */
+    int max_pages;               /* entries of a row of page_table */
+    const int32_t *cu_new;       /* device [n_seq + 1], or NULL */
+    const int32_t *kv_len;       /* device [n_seq]: tokens of the sequence, the new ones included */
+    const int32_t *page_table;   /* device [n_seq][max_pages] */
+} prox_kv_seqs;
+
+/*
+ * Rotation of queries and keys by their positions: the pair (a, b) of frequency
+ * i becomes (a cos - b sin, a sin + b cos), computed in 64 bits, rounded to 32 bits
+ * and then to the dtype.  table: device fp32 [n_pos][dim], 16-byte aligned: row
+ * p holds the dim / 2 cosines of position p, then the sines.  Pairs: channels
+ * (i, i + dim / 2), or (2 i, 2 i + 1) if interleaved; channels from dim on stay.
+ */
+typedef struct {
+    const float *table;
+    int n_pos;         /* >= the call's max_kv */
+    int dim;           /* a multiple of 16, at most head_dim */
+    int interleaved;
+} prox_rope;
+
+/*
+ * Append the new tokens' keys and values to the cache, in one launch with the
+ * rotation of keys and queries.
+ *   k, v   device, token t's head h at k + t * ldk + h * head_dim (16-byte aligned;
+ *          ldk, ldv multiples of 8, >= kv_heads * head_dim)
+ *   q      device, likewise with q_heads, or NULL (then q_out is NULL)
+ *   q_out  device, the rotated queries (may be q itself, with ldq_out = ldq)
+ *   rope   NULL: no rotation (q is copied)
+ * q, k, v may be parts of one tensor.  Every other token of the cache keeps its
+ * codes.  Rows without a place are not written to q_out.
+ */
+prox_status prox_kv_append(const prox_kv_cache *c, const prox_kv_seqs *s, const void *k, int64_t ldk,
+                           const void *v, int64_t ldv, const void *q, int q_heads, int64_t ldq,
+                           void *q_out, int64_t ldq_out, const prox_rope *rope, hipStream_t stream);
+
+/* What the cache holds of the call's tokens, for inspection and tests: sigma c
+ * in fp32, device [n_tokens][kv_heads][head_dim] each (16-byte aligned).  Rows
+ * without a place are not written. */
+prox_status prox_kv_read(const prox_kv_cache *c, const prox_kv_seqs *s, float *k, float *v,
+                         hipStream_t stream);
+
+/*
+ * Attention of the new tokens over the cache (which holds them already):
+ *   out[t][h] = sum_p softmax_p(scale q[t][h] . k[p][h']) v[p][h'],
+ *   h' = h / (q_heads / kv_heads),
+ * over the positions p of the token's sequence up to its own and, with window >
+ * 0, only the last `window` of them (its own included).  Scores, softmax and sums
+ * in fp32, out rounded once to the dtype.  Rows without a place, and rows that
+ * see no position, get 0.
+ *   q, out  device, token t's head h at q + t * ldq + h * head_dim (16-byte aligned;
+ *           ldq, ldo multiples of 8, >= q_heads * head_dim); out may be q with ldo = ldq
+ *   q_heads a multiple of kv_heads
+ *   ws      device, 256-byte aligned, ws_bytes >= prox_kv_attn_workspace_bytes(),
+ *           one size for every call with this head_dim; needs no initialisation
+ * Results are the same for every run, and depend on max_kv and max_new only in
+ * fp32 summation order.
+ */
+size_t prox_kv_attn_workspace_bytes(int head_dim);
+prox_status prox_kv_attn(const prox_kv_cache *c, const prox_kv_seqs *s, const void *q, int q_heads,
+                         int64_t ldq, float scale, int window, void *out, int64_t ldo, void *ws,
+                         size_t ws_bytes, hipStream_t stream);
+
 /* Static description of a status code. */
 const char *prox_strerror(prox_status status);
 

@@ -120,4 +120,27 @@ hipError_t launch_reduce(int dtype, const float *ypart, int nwg, int nb, int d, 
 hipError_t launch_add_rmsnorm(int dtype, const void *x, const void *y, int batch, int d, float eps,
                               void *out, hipStream_t stream);
 
+
+// Projections on INT4 weights (LinearLayout).
+hipError_t launch_pack_linear(int dtype, const void *w, int n, int k, int group, void *blob,
+                              hipStream_t stream);
+hipError_t launch_unpack_linear(const void *blob, int n, int k, int group, int8_t *codes,
+                                uint16_t *scales, hipStream_t stream);
+hipError_t launch_linear(int dtype, const void *blob, int n, int k, int group, const void *x,
+                         int64_t ldx, int batch, const void *bias, void *y, int64_t ldy,
+                         hipStream_t stream);
+
+struct Rope {
+    const float *table;   // NULL: no rotation
+    int dim, interleaved;
+};
+
+hipError_t launch_kv_append(int dtype, const KvCache &c, const KvSeqs &s, const void *k, int64_t ldk,
+                            const void *v, int64_t ldv, const void *q, int q_heads, int64_t ldq,
+                            void *q_out, int64_t ldq_out, const Rope &rope, hipStream_t stream);
+hipError_t launch_kv_read(const KvCache &c, const KvSeqs &s, float *k, float *v, hipStream_t stream);
+hipError_t launch_attn(int dtype, const KvCache &c, const KvSeqs &s, const void *q, int q_heads,
+                       int64_t ldq, float scale, int window, void *out, int64_t ldo, void *ws,
+                       hipStream_t stream);
+
 }  // namespace prox

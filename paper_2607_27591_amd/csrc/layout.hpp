@@ -221,4 +221,105 @@ __host__ __device__ inline size_t ws_bytes_up_to(int d, int f, int batch, int wq
     return own.total + (y_vec > y_own ? y_vec - y_own : 0);
 }
 
+// ---------------------------------------------------------------------------
+// Projections on INT4 weights
+// ---------------------------------------------------------------------------
+// codes   [row tile of 16][block of 128 inputs][lane 0..63][4 words]: lane l holds row
+//         l % 16 of the tile, word i the codes (q + 8) of inputs 32 i + 8 (l / 16) ..
+//         + 7 of the block, in the order of kNibble: a lane's word is its operand of
+//         one 16 x 16 x 32 MFMA, and a wave's load of a block one run of 1024 bytes.
+//         Rows past n and inputs past k hold code 0 (q + 8 = 8).
+// scales  (256-aligned) [row tile][k / group][16] fp16 bits, 0 past n.
+constexpr int kLinearRows = 16;
+constexpr int kLinearBlock = 128;
+
+// Nibble of element e (0..7) of a code word: pairs (2 p, 2 p + 1) stand 16 bits apart, so
+// that one shift and one and-or make a register of two 16-bit operands.
+__host__ __device__ constexpr int nibble_of(int e) { return (e >> 1) + 4 * (e & 1); }
+
+struct LinearLayout {
+    int tiles, blocks, groups;
+    size_t scales, total;
+    __host__ __device__ LinearLayout(int n, int k, int group)
+        : tiles((n + kLinearRows - 1) / kLinearRows), blocks((k + kLinearBlock - 1) / kLinearBlock),
+          groups(k / group) {
+        scales = (size_t)tiles * blocks * 1024;
+        total = align_up(scales + (size_t)tiles * groups * kLinearRows * 2, 256);
+    }
+};
+
+// ---------------------------------------------------------------------------
+// 4-bit paged key/value cache
+// ---------------------------------------------------------------------------
+// [page][kv head][block of 32 tokens of the page] records, each of
+//   K codes   [token / 16][lane 0..63][D / 32 words]: lane l holds token l % 16 of the
+//             half block, word i channels 32 i + 8 (l / 16) .. + 7 (nibble_of)
+//   V codes   [lane 0..63][D / 16 words]: lane l, word i holds channel 16 i + l % 16, at
+//             nibble j token 4 (l / 16) + j (j < 4), 16 + 4 (l / 16) + j - 4 (j >= 4)
+//   K scales  [group][kv_slot(token)] fp16 bits;   V scales alike
+// so that a lane's words are its MFMA operands of both products (queries times keys, and
+// values times probabilities as the first product leaves them), its four runs of scales
+// those of the tokens whose scores it gets, and a record one contiguous run.
+constexpr int kKvBlock = 32;
+
+// Place of token t of a block in a row of scales: the 8 tokens of lanes 16 h .. 16 h + 15 together.
+__host__ __device__ constexpr int kv_slot(int t) { return ((t >> 2) & 3) * 8 + (t >> 4) * 4 + (t & 3); }
+
+struct KvLayout {
+    int groups;
+    size_t v_codes, k_scales, v_scales, record;   // offsets in a record, its bytes
+    __host__ __device__ constexpr KvLayout(int head_dim, int group)
+        : groups(head_dim / group), v_codes((size_t)16 * head_dim), k_scales((size_t)32 * head_dim),
+          v_scales((size_t)32 * head_dim + (size_t)groups * 64),
+          record((size_t)32 * head_dim + (size_t)groups * 128) {}
+};
+
+// The 4-bit paged cache (KvLayout) and the sequences of a call, as the kernels take them.
+struct KvCache {
+    uint8_t *blob;
+    int heads, dim, group, page_size, n_pages;
+    size_t page_bytes;
+};
+struct KvSeqs {
+    const int32_t *cu, *len, *table;
+    int n_seq, max_new, n_tokens, max_kv, max_pages;
+};
+// New tokens of sequence s: rows t0 .. t0 + n - 1 (of m, the first max_new), row i at
+// position pos0 + i (negative: no place); len tokens in the cache.
+struct SeqTokens {
+    int t0, n, pos0, len;
+};
+__host__ __device__ inline int clamp_int(int v, int hi) { return v < 0 ? 0 : v > hi ? hi : v; }
+__host__ __device__ inline SeqTokens seq_tokens(const KvSeqs &q, int s) {
+    SeqTokens r;
+    int m = q.max_new;
+    if (q.cu) {
+        r.t0 = clamp_int(q.cu[s], q.n_tokens);
+        const int t1 = clamp_int(q.cu[s + 1], q.n_tokens);
+        m = t1 > r.t0 ? t1 - r.t0 : 0;
+    } else {
+        r.t0 = s * q.max_new;
+    }
+    r.n = m < q.max_new ? m : q.max_new;
+    r.len = clamp_int(q.len[s], q.max_kv);
+    r.pos0 = r.len - m;
+    return r;
+}
+// Record of the block of 32 tokens that starts at position 32 b of sequence s for a
+// head, or NULL when its page lies outside the cache.  32 b < max_pages * page_size.
+__host__ __device__ inline uint8_t *kv_record(const KvCache &c, const KvSeqs &q, size_t record, int s,
+                                              int head, int b) {
+    const int per = c.page_size / kKvBlock, page = b / per;
+    const int id = q.table[(size_t)s * q.max_pages + page];
+    if (id < 0 || id >= c.n_pages) return nullptr;
+    return c.blob + (size_t)id * c.page_bytes + ((size_t)head * per + (b - page * per)) * record;
+}
+
+// Split of attention over a long cache: a call's partial results, one row of head_dim
+// accumulators with its maximum and sum per (query row, split), at most kAttnPartRows.
+constexpr int kAttnPartRows = 16384;
+__host__ __device__ inline size_t attn_workspace_bytes(int head_dim) {
+    return (size_t)kAttnPartRows * (size_t)(head_dim + 2) * 4;
+}
+
 }  // namespace prox

@@ -1,0 +1,129 @@
+// Projections on INT4 weights with group scales: packing, its inverse view, and
+// y = x W^T (+ bias) for up to 64 rows.
+#include "common.hpp"
+#include "kernels.hpp"
+#include "quant.hpp"
+
+namespace prox {
+
+// Packing: a workgroup takes the 16 rows of a tile over one unit of inputs (a group,
+// at least 128), 16 lanes a row, so that it writes whole blocks of 1024 bytes.  A unit of
+// 128 is read once, a longer group twice.  Bound by HBM (weights read once).
+template <int DT>
+__global__ __launch_bounds__(256) void pack_linear_kernel(const uint16_t *__restrict__ w, int n, int k,
+                                                          int group, uint8_t *__restrict__ blob) {
+    const LinearLayout L(n, k, group);
+    const int tile = blockIdx.x, l = threadIdx.x % 16, r = threadIdx.x / 16;
+    const int unit = group > kLinearBlock ? group : kLinearBlock;
+    const int first = (int)blockIdx.y * unit;
+    const int j = tile * kLinearRows + r;
+    const uint16_t *src = w + (size_t)j * k;
+    uint16_t *scales = reinterpret_cast<uint16_t *>(blob + L.scales) + (size_t)tile * L.groups * kLinearRows + r;
+    auto load = [&](int i) {   // past the matrix: zeros
+        return j < n && i < k ? *reinterpret_cast<const uint4 *>(src + i) : make_uint4(0, 0, 0, 0);
+    };
+    const int span = group < kLinearBlock ? group / 8 : 16;   // lanes of a group
+    uint4 v = load(first + 8 * l);
+    uint32_t a = abs_max8<DT>(v);
+    for (int i = kLinearBlock; i < unit; i += kLinearBlock) a = max(a, abs_max8<DT>(load(first + i + 8 * l)));
+    for (int m = 1; m < span; m <<= 1) a = max(a, (uint32_t)__shfl_xor((int)a, m));
+    const GroupScale s = group_scale<DT>(a, 7);
+    const int g = (first + 8 * l) / group;
+    if (l % span == 0 && g < L.groups) scales[(size_t)g * kLinearRows] = s.bits;
+    for (int i = 0; i < unit; i += kLinearBlock) {
+        if (i > 0) v = load(first + i + 8 * l);
+        uint32_t word = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            int q = quantise<DT>(half_of(v, e), s.sigma, s.inv, 7.0f);
+            if (s.sigma == 0.0f) q = 0;   // a NaN weight too
+            word |= (uint32_t)(q + 8) << (4 * nibble_of(e));
+        }
+        const size_t blk = (size_t)tile * L.blocks + (first + i) / kLinearBlock;
+        *reinterpret_cast<uint32_t *>(blob + blk * 1024 + (size_t)((l % 4) * 16 + r) * 16 + (l / 4) * 4) = word;
+    }
+}
+
+// Inverse view: one thread per (row, 8 inputs).
+__global__ __launch_bounds__(256) void unpack_linear_kernel(const uint8_t *__restrict__ blob, int n, int k,
+                                                            int group, int8_t *__restrict__ codes,
+                                                            uint16_t *__restrict__ scales) {
+    const LinearLayout L(n, k, group);
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int per = k / 8;
+    if (id >= (long long)n * per) return;
+    const int j = (int)(id / per), ch = (int)(id % per);
+    const int c = ch % 16;   // chunk of the block
+    const size_t blk = (size_t)(j / kLinearRows) * L.blocks + ch / 16;
+    const uint32_t word = *reinterpret_cast<const uint32_t *>(
+        blob + blk * 1024 + (size_t)((c % 4) * 16 + j % kLinearRows) * 16 + (c / 4) * 4);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) codes[id * 8 + e] = (int8_t)((int)((word >> (4 * nibble_of(e))) & 15) - 8);
+    const int g = ch * 8 / group;
+    if (ch * 8 % group == 0)
+        scales[(size_t)j * L.groups + g] = reinterpret_cast<const uint16_t *>(
+            blob + L.scales)[((size_t)(j / kLinearRows) * L.groups + g) * kLinearRows + j % kLinearRows];
+}
+
+// One wave per output, one row of x after another.
+template <int DT>
+__global__ __launch_bounds__(256) void linear_kernel(const uint8_t *__restrict__ blob, int n, int k, int group,
+                                                     const uint16_t *__restrict__ x, int64_t ldx, int batch,
+                                                     const uint16_t *__restrict__ bias, uint16_t *__restrict__ y,
+                                                     int64_t ldy) {
+    const LinearLayout L(n, k, group);
+    const int j = blockIdx.x * 4 + threadIdx.x / kWave, lane = lane_id();
+    if (j >= n) return;
+    const uint16_t *scales = reinterpret_cast<const uint16_t *>(blob + L.scales) +
+                             (size_t)(j / kLinearRows) * L.groups * kLinearRows + j % kLinearRows;
+    for (int b = 0; b < batch; ++b) {
+        float acc = 0.0f;
+        for (int ch = lane; ch < k / 8; ch += kWave) {
+            const int c = ch % 16;
+            const uint32_t word = *reinterpret_cast<const uint32_t *>(
+                blob + ((size_t)(j / kLinearRows) * L.blocks + ch / 16) * 1024 +
+                (size_t)((c % 4) * 16 + j % kLinearRows) * 16 + (c / 4) * 4);
+            const uint4 v = *reinterpret_cast<const uint4 *>(x + (size_t)b * ldx + (size_t)ch * 8);
+            float s = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                s = fmaf((float)((int)((word >> (4 * nibble_of(e))) & 15) - 8),
+                         half_to_float<DT>((uint16_t)half_of(v, e)), s);
+            acc = fmaf(s, f16_bits_to_float(scales[(size_t)(ch * 8 / group) * kLinearRows]), acc);
+        }
+        acc = wave_sum(acc);
+        if (lane == 0) y[(size_t)b * ldy + j] = float_to_half<DT>(acc + (bias ? half_to_float<DT>(bias[j]) : 0.0f));
+    }
+}
+
+hipError_t launch_pack_linear(int dtype, const void *w, int n, int k, int group, void *blob, hipStream_t s) {
+    const LinearLayout L(n, k, group);
+    const int unit = group > kLinearBlock ? group : kLinearBlock;
+    const dim3 grid((unsigned)L.tiles, (unsigned)((k + unit - 1) / unit));
+    auto *wp = static_cast<const uint16_t *>(w);
+    auto *b = static_cast<uint8_t *>(blob);
+    if (dtype == kBF16) pack_linear_kernel<kBF16><<<grid, 256, 0, s>>>(wp, n, k, group, b);
+    else pack_linear_kernel<kF16><<<grid, 256, 0, s>>>(wp, n, k, group, b);
+    return hipGetLastError();
+}
+
+hipError_t launch_unpack_linear(const void *blob, int n, int k, int group, int8_t *codes, uint16_t *scales,
+                                hipStream_t s) {
+    const long long blocks = ((long long)n * (k / 8) + 255) / 256;
+    unpack_linear_kernel<<<(unsigned)blocks, 256, 0, s>>>(static_cast<const uint8_t *>(blob), n, k, group, codes, scales);
+    return hipGetLastError();
+}
+
+hipError_t launch_linear(int dtype, const void *blob, int n, int k, int group, const void *x, int64_t ldx, int batch,
+                         const void *bias, void *y, int64_t ldy, hipStream_t s) {
+    auto *bl = static_cast<const uint8_t *>(blob);
+    auto *xp = static_cast<const uint16_t *>(x);
+    auto *bp = static_cast<const uint16_t *>(bias);
+    auto *yp = static_cast<uint16_t *>(y);
+    const unsigned grid = (unsigned)((n + 3) / 4);
+    if (dtype == kBF16) linear_kernel<kBF16><<<grid, 256, 0, s>>>(bl, n, k, group, xp, ldx, batch, bp, yp, ldy);
+    else linear_kernel<kF16><<<grid, 256, 0, s>>>(bl, n, k, group, xp, ldx, batch, bp, yp, ldy);
+    return hipGetLastError();
+}
+
+}  // namespace prox

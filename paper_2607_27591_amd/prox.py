@@ -53,6 +53,28 @@ class _W4(ctypes.Structure):
                 ("bytes", ctypes.c_size_t)]
 
 
+class _W4Linear(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("n", ctypes.c_int), ("k", ctypes.c_int),
+                ("group", ctypes.c_int), ("blob", ctypes.c_void_p), ("bytes", ctypes.c_size_t)]
+
+
+class _KVCache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("group", ctypes.c_int), ("page_size", ctypes.c_int), ("n_pages", ctypes.c_int),
+                ("blob", ctypes.c_void_p), ("bytes", ctypes.c_size_t)]
+
+
+class _KVSeqs(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int), ("max_new", ctypes.c_int), ("n_tokens", ctypes.c_int),
+                ("max_kv", ctypes.c_int), ("max_pages", ctypes.c_int), ("cu_new", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("n_pos", ctypes.c_int), ("dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int)]
+
+
 _lib = None
 
 
@@ -102,13 +124,28 @@ def lib() -> ctypes.CDLL:
         L.prox_ffn_dense_w4.argtypes = [QP, P, I, P, P, S, P]
         L.prox_ffn_sparse_w4.argtypes = [QP, PP, P, I, I, I, P, P, P, P, P, S, P, P]
         L.prox_ffn_sparse_tau_w4.argtypes = [QP, PP, P, I, Z, Z, P, P, P, P, P, P, S, P]
+        LP, CP, KP, RP = (ctypes.POINTER(t) for t in (_W4Linear, _KVCache, _KVSeqs, _Rope))
+        N = ctypes.c_int64
+        L.prox_linear_w4_bytes.argtypes = [I, I, I]
+        L.prox_linear_w4_bytes.restype = S
+        L.prox_pack_linear_w4.argtypes = [P, LP, P]
+        L.prox_unpack_linear_w4.argtypes = [LP, P, P, P]
+        L.prox_linear_w4.argtypes = [LP, P, N, I, P, P, N, P]
+        L.prox_kv_bytes.argtypes = [I, I, I, I, I]
+        L.prox_kv_bytes.restype = S
+        L.prox_kv_append.argtypes = [CP, KP, P, N, P, N, P, I, N, P, N, RP, P]
+        L.prox_kv_read.argtypes = [CP, KP, P, P, P]
+        L.prox_kv_attn_workspace_bytes.argtypes = [I]
+        L.prox_kv_attn_workspace_bytes.restype = S
+        L.prox_kv_attn.argtypes = [CP, KP, P, I, N, Z, I, P, N, P, S, P]
         L.prox_strerror.argtypes = [I]
         L.prox_strerror.restype = ctypes.c_char_p
         for name in ("prox_pack_proxy", "prox_unpack_proxy", "prox_ffn_dense", "prox_ffn_sparse",
                      "prox_ffn_sparse_staged", "prox_ffn_sparse_tau", "prox_add_rmsnorm",
                      "prox_reservoir_add", "prox_quantile_threshold", "prox_allocate_sparsity",
                      "prox_pack_w4", "prox_unpack_w4", "prox_ffn_dense_w4", "prox_ffn_sparse_w4",
-                     "prox_ffn_sparse_tau_w4"):
+                     "prox_ffn_sparse_tau_w4", "prox_pack_linear_w4", "prox_unpack_linear_w4",
+                     "prox_linear_w4", "prox_kv_append", "prox_kv_read", "prox_kv_attn"):
             getattr(L, name).restype = I
         _lib = L
     return _lib
@@ -510,6 +547,273 @@ def add_rmsnorm(x: torch.Tensor, y: torch.Tensor, eps: float = 1e-6,
     _check(lib().prox_add_rmsnorm(_ptr(x), _ptr(y), x2.shape[0], x2.shape[1], dt,
                                   ctypes.c_float(eps), _ptr(out), _stream(x.device)),
            "prox_add_rmsnorm")
+    return out
+
+
+# ---------------------------------------------------------------------------
+# The attention half of a decoder layer
+# ---------------------------------------------------------------------------
+
+def _on(device: torch.device, f, *args) -> int:
+    """f(*args, stream) on the current stream of `device`, which may not be the
+    current device."""
+    if device.index is None or device.index == torch.cuda.current_device():
+        return f(*args, _stream(device))
+    with torch.cuda.device(device):
+        return f(*args, _stream(device))
+
+
+def _same_device(device: torch.device, **tensors) -> None:
+    for what, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{what} is on {t.device}, not on {device}")
+
+
+@dataclasses.dataclass
+class LinearW4:
+    """A projection's weights in INT4 (W4A16): an opaque device blob."""
+    blob: torch.Tensor
+    dtype: torch.dtype
+    n: int
+    k: int
+    group: int
+
+    def struct(self) -> _W4Linear:
+        _dev_tensor(self.blob, "linear blob", torch.uint8)
+        return _W4Linear(_TORCH_DT[self.dtype], self.n, self.k, self.group, self.blob.data_ptr(),
+                         self.blob.numel())
+
+
+def linear_w4_bytes(n: int, k: int, group: int = 128) -> int:
+    return int(lib().prox_linear_w4_bytes(n, k, group))
+
+
+def pack_linear_w4(w: torch.Tensor, group: int = 128) -> LinearW4:
+    """Quantise nn.Linear's weight w [n][k] (float16 or bfloat16)."""
+    if w.dtype not in _TORCH_DT:
+        raise ValueError("weights must be float16 or bfloat16")
+    _dev_tensor(w, "w")
+    if w.dim() != 2:
+        raise ValueError("w must be [n][k]")
+    n, k = w.shape
+    size = linear_w4_bytes(n, k, group)
+    if size == 0:
+        raise ProxError(2, "prox_linear_w4_bytes")
+    q = LinearW4(torch.empty(size, dtype=torch.uint8, device=w.device), w.dtype, n, k, group)
+    qs = q.struct()
+    _check(_on(w.device, lib().prox_pack_linear_w4, _ptr(w), ctypes.byref(qs)), "prox_pack_linear_w4")
+    return q
+
+
+def unpack_linear_w4(q: LinearW4):
+    """(codes int8 [n][k], scales fp16 bits int16 [n][k / group])."""
+    dev = q.blob.device
+    codes = torch.empty((q.n, q.k), dtype=torch.int8, device=dev)
+    scales = torch.empty((q.n, q.k // q.group), dtype=torch.int16, device=dev)
+    qs = q.struct()
+    _check(_on(dev, lib().prox_unpack_linear_w4, ctypes.byref(qs), _ptr(codes), _ptr(scales)),
+           "prox_unpack_linear_w4")
+    return codes, scales
+
+
+def _rows2(t: torch.Tensor, what: str, dtype: torch.dtype, cols: int) -> int:
+    """Row stride of a [rows][cols] device tensor whose rows may stand apart."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError(f"{what} must be a CUDA (HIP) tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{what} must have dtype {dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be [rows][{cols}] with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else cols
+
+
+def linear_w4(q: LinearW4, x: torch.Tensor, bias: Optional[torch.Tensor] = None,
+              y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [batch][k] (or [k]) times the INT4 weights, plus bias [n]; rows of x and y may
+    stand apart (parts of wider tensors)."""
+    x2 = x.unsqueeze(0) if x.dim() == 1 else x
+    ldx = _rows2(x2, "x", q.dtype, q.k)
+    if y is None:
+        y = torch.empty(x.shape[:-1] + (q.n,), dtype=q.dtype, device=x.device)
+    y2 = y.unsqueeze(0) if y.dim() == 1 else y
+    ldy = _rows2(y2, "y", q.dtype, q.n)
+    if y2.shape[0] != x2.shape[0]:
+        raise ValueError("y must have the rows of x")
+    if bias is not None:
+        _dev_tensor(bias, "bias", q.dtype)
+        if bias.numel() != q.n:
+            raise ValueError("bias must be [n]")
+    _same_device(x.device, blob=q.blob, y=y, bias=bias)
+    qs = q.struct()
+    _check(_on(x.device, lib().prox_linear_w4, ctypes.byref(qs), _ptr(x), ldx, x2.shape[0], _ptr(bias),
+               _ptr(y), ldy), "prox_linear_w4")
+    return y
+
+
+@dataclasses.dataclass
+class KVCache:
+    """Paged key/value cache in 4 bits: an opaque device blob."""
+    blob: torch.Tensor
+    dtype: torch.dtype
+    kv_heads: int
+    head_dim: int
+    group: int
+    page_size: int
+    n_pages: int
+
+    def struct(self) -> _KVCache:
+        _dev_tensor(self.blob, "cache blob", torch.uint8)
+        return _KVCache(_TORCH_DT[self.dtype], self.kv_heads, self.head_dim, self.group, self.page_size,
+                        self.n_pages, self.blob.data_ptr(), self.blob.numel())
+
+
+def kv_bytes(kv_heads: int, head_dim: int, group: int, page_size: int, n_pages: int) -> int:
+    return int(lib().prox_kv_bytes(kv_heads, head_dim, group, page_size, n_pages))
+
+
+def new_kv_cache(n_pages: int, page_size: int, kv_heads: int, head_dim: int, dtype: torch.dtype,
+                 group: int = 64, device="cuda") -> KVCache:
+    if dtype not in _TORCH_DT:
+        raise ValueError("dtype must be float16 or bfloat16")
+    n = kv_bytes(kv_heads, head_dim, group, page_size, n_pages)
+    if n == 0:
+        raise ProxError(2, "prox_kv_bytes")
+    return KVCache(torch.empty(n, dtype=torch.uint8, device=device), dtype, kv_heads, head_dim, group,
+                   page_size, n_pages)
+
+
+@dataclasses.dataclass
+class KVSeqs:
+    """The sequences of a call (prox_kv_seqs): device int32 kv_len [n_seq] (the new
+    tokens included), page_table [n_seq][max_pages] and, where sequences have unequal
+    numbers of new tokens (at most max_new), cu_new [n_seq + 1].  max_kv bounds kv_len
+    (0: what the page table holds)."""
+    kv_len: torch.Tensor
+    page_table: torch.Tensor
+    max_new: int = 1
+    cu_new: Optional[torch.Tensor] = None
+    max_kv: int = 0
+
+    def struct(self, n_tokens: int) -> _KVSeqs:
+        _dev_tensor(self.kv_len, "kv_len", torch.int32)
+        _dev_tensor(self.page_table, "page_table", torch.int32)
+        n = self.kv_len.numel()
+        if self.page_table.dim() != 2 or self.page_table.shape[0] != n:
+            raise ValueError("page_table must be [n_seq][max_pages]")
+        if self.cu_new is not None:
+            _dev_tensor(self.cu_new, "cu_new", torch.int32)
+            if self.cu_new.numel() != n + 1:
+                raise ValueError("cu_new must be [n_seq + 1]")
+        return _KVSeqs(n, self.max_new, n_tokens, self.max_kv, self.page_table.shape[1],
+                       None if self.cu_new is None else self.cu_new.data_ptr(), self.kv_len.data_ptr(),
+                       self.page_table.data_ptr())
+
+
+@dataclasses.dataclass
+class Rope:
+    """Rotation table, device float32 [n_pos][dim]: dim / 2 cosines, then the sines, of
+    every position; pairs (i, i + dim / 2), or (2 i, 2 i + 1) if interleaved."""
+    table: torch.Tensor
+    interleaved: bool = False
+
+    def struct(self) -> _Rope:
+        _dev_tensor(self.table, "rope table", torch.float32)
+        if self.table.dim() != 2:
+            raise ValueError("rope table must be [n_pos][dim]")
+        return _Rope(self.table.data_ptr(), self.table.shape[0], self.table.shape[1], int(self.interleaved))
+
+
+def _heads(t: torch.Tensor, what: str, c: KVCache, heads: Optional[int] = None) -> int:
+    """Token stride of a [tokens][heads][head_dim] device tensor."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError(f"{what} must be a CUDA (HIP) tensor")
+    if t.dtype != c.dtype:
+        raise ValueError(f"{what} must have dtype {c.dtype}, got {t.dtype}")
+    if (t.dim() != 3 or t.shape[2] != c.head_dim or (heads is not None and t.shape[1] != heads) or
+            t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != c.head_dim)):
+        raise ValueError(f"{what} must be [tokens][{'heads' if heads is None else heads}][{c.head_dim}] "
+                         "with the heads of a token contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * c.head_dim
+
+
+def kv_append(c: KVCache, s: KVSeqs, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+              q_out: Optional[torch.Tensor] = None, rope: Optional[Rope] = None) -> Optional[torch.Tensor]:
+    """Append the new tokens' k and v [tokens][kv_heads][head_dim] to the cache, rotated by
+    rope if given.  Returns the rotated queries (q_out, which may be q; made here when
+    not given), None without q."""
+    T = k.shape[0]
+    ldk, ldv = _heads(k, "k", c, c.kv_heads), _heads(v, "v", c, c.kv_heads)
+    if v.shape[0] != T:
+        raise ValueError("v must have the tokens of k")
+    ldq = ldo = heads = 0
+    if q is not None:
+        ldq, heads = _heads(q, "q", c), q.shape[1]
+        if q_out is None:   # rows without a place are not written
+            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        ldo = _heads(q_out, "q_out", c, heads)
+        if q.shape[0] != T or q_out.shape[0] != T:
+            raise ValueError("q and q_out must have the tokens of k")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _same_device(k.device, blob=c.blob, v=v, q=q, q_out=q_out, kv_len=s.kv_len, page_table=s.page_table,
+                 cu_new=s.cu_new, rope=None if rope is None else rope.table)
+    cs, ss = c.struct(), s.struct(T)
+    rs = None if rope is None else ctypes.byref(rope.struct())
+    _check(_on(k.device, lib().prox_kv_append, ctypes.byref(cs), ctypes.byref(ss), _ptr(k), ldk, _ptr(v), ldv,
+               _ptr(q), heads, ldq, _ptr(q_out), ldo, rs), "prox_kv_append")
+    return q_out
+
+
+def kv_read(c: KVCache, s: KVSeqs, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+            n_tokens: Optional[int] = None):
+    """(k, v) float32 [n_tokens][kv_heads][head_dim]: what the cache holds of the call's
+    tokens.  n_tokens: needed with cu_new when neither k nor v is given."""
+    if n_tokens is None:
+        given = k if k is not None else v
+        if given is None and s.cu_new is not None:
+            raise ValueError("n_tokens is needed")
+        n_tokens = s.kv_len.numel() * s.max_new if given is None else given.shape[0]
+    shape = (n_tokens, c.kv_heads, c.head_dim)
+    dev = c.blob.device
+    k = torch.zeros(shape, dtype=torch.float32, device=dev) if k is None else _dev_tensor(k, "k", torch.float32)
+    v = torch.zeros(shape, dtype=torch.float32, device=dev) if v is None else _dev_tensor(v, "v", torch.float32)
+    if tuple(k.shape) != shape or tuple(v.shape) != shape:
+        raise ValueError("k and v must be [n_tokens][kv_heads][head_dim]")
+    _same_device(dev, k=k, v=v, kv_len=s.kv_len, page_table=s.page_table, cu_new=s.cu_new)
+    cs, ss = c.struct(), s.struct(n_tokens)
+    _check(_on(dev, lib().prox_kv_read, ctypes.byref(cs), ctypes.byref(ss), _ptr(k), _ptr(v)), "prox_kv_read")
+    return k, v
+
+
+def kv_attn_workspace_bytes(head_dim: int) -> int:
+    return int(lib().prox_kv_attn_workspace_bytes(head_dim))
+
+
+def new_kv_attn_workspace(head_dim: int, device="cuda") -> torch.Tensor:
+    n = kv_attn_workspace_bytes(head_dim)
+    if n == 0:
+        raise ProxError(2, "prox_kv_attn_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def kv_attn(c: KVCache, s: KVSeqs, q: torch.Tensor, scale: Optional[float] = None, window: int = 0,
+            out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new tokens' queries [tokens][q_heads][head_dim] over the cache
+    (which holds the tokens' own keys and values already).  scale: head_dim ** -0.5 when
+    not given; window > 0: the last `window` positions only."""
+    ldq = _heads(q, "q", c)
+    if out is None:   # rows of no sequence are not written
+        out = (torch.empty if s.cu_new is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+    ldo = _heads(out, "out", c, q.shape[1])
+    if out.shape[0] != q.shape[0]:
+        raise ValueError("out must have the tokens of q")
+    ws = new_kv_attn_workspace(c.head_dim, q.device) if ws is None else _dev_tensor(ws, "ws", torch.uint8)
+    _same_device(q.device, blob=c.blob, out=out, ws=ws, kv_len=s.kv_len, page_table=s.page_table,
+                 cu_new=s.cu_new)
+    cs, ss = c.struct(), s.struct(q.shape[0])
+    _check(_on(q.device, lib().prox_kv_attn, ctypes.byref(cs), ctypes.byref(ss), _ptr(q), q.shape[1], ldq,
+               c.head_dim ** -0.5 if scale is None else float(scale), int(window), _ptr(out), ldo, _ptr(ws),
+               ws.numel()), "prox_kv_attn")
     return out
 
 
