@@ -175,6 +175,41 @@ __device__ __forceinline__ v4f mfma4(uint2 a, uint2 b, v4f c) {
                                                   __builtin_bit_cast(v4h, b), c, 0, 0, 0);
 }
 
+// The same, 16 x 16 x 32: lane l holds A[l % 16][8 (l / 16) + e] and B[8 (l / 16) + e][l % 16]
+// for e = 0..7 (eight 16-bit values in a uint4) and gets D[4 (l / 16) + e][l % 16].
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+template <int DT>
+__device__ __forceinline__ v4f mfma32(uint4 a, uint4 b, v4f c) {
+    if constexpr (DT == kBF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+
+// A word of 8 codes (q + 8, in the order of nibble_of) as an operand of mfma32: exact
+// 16-bit values under an exponent, bf16 16 + n and fp16 64 + n (as Int4Quad), 8 and 7
+// instructions.  bias comes off with the sum of the other operand: minus() is the operand
+// of a product that gives it.
+template <int DT>
+struct Int4Oct {
+    static constexpr float bias = DT == kBF16 ? 24.0f : 72.0f;
+    static constexpr bool kB = DT == kBF16;
+    uint32_t mask = kB ? 0x00780078u : 0x00F000F0u;
+    uint32_t M = kB ? 0x41804180u : 0x54005400u;
+    __device__ __forceinline__ Int4Oct() { asm("" : "+s"(mask), "+v"(M)); }   // kept as one v_and_or_b32
+    __device__ __forceinline__ uint4 operator()(uint32_t w) const {
+        if constexpr (kB)
+            return make_uint4(((w << 3) & mask) | M, ((w >> 1) & mask) | M, ((w >> 5) & mask) | M, ((w >> 9) & mask) | M);
+        else
+            return make_uint4(((w << 4) & mask) | M, (w & mask) | M, ((w >> 4) & mask) | M, ((w >> 8) & mask) | M);
+    }
+    static __device__ __forceinline__ uint4 minus() {
+        const uint32_t m = kB ? 0xC1C0C1C0u : 0xD480D480u;
+        return make_uint4(m, m, m, m);
+    }
+};
+
 // 16- and 8-byte streaming loads (non-temporal hint: weights are read once
 // per call).
 __device__ __forceinline__ uint4 load_stream16(const void *p) {
