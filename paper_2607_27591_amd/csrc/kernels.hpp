@@ -126,6 +126,20 @@ hipError_t launch_pack_linear(int dtype, const void *w, int n, int k, int group,
                               hipStream_t stream);
 hipError_t launch_unpack_linear(const void *blob, int n, int k, int group, int8_t *codes,
                                 uint16_t *scales, hipStream_t stream);
+struct LinearArgs {
+    const uint8_t *blob;
+    int n, k, group;
+    const uint16_t *x;
+    int64_t ldx;
+    int batch;
+    const uint16_t *bias;
+    uint16_t *y;
+    int64_t ldy;
+    uint32_t per_group;   // ceil(2^20 / (group / 128)): b * per_group >> 20 is block b's group (b <= 512)
+};
+
+hipError_t launch_linear_bf16(const LinearArgs &a, hipStream_t stream);
+hipError_t launch_linear_f16(const LinearArgs &a, hipStream_t stream);
 hipError_t launch_linear(int dtype, const void *blob, int n, int k, int group, const void *x,
                          int64_t ldx, int batch, const void *bias, void *y, int64_t ldy,
                          hipStream_t stream);

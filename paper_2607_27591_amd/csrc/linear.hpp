@@ -1,0 +1,241 @@
+// Projections on INT4 weights with group scales, y = x W^T (+ bias) for up to 64 rows: the
+// kernel, and its variant by shape.  Compiled once per dtype (linear_f16.hip,
+// linear_bf16.hip).
+#pragma once
+
+#include "common.hpp"
+#include "kernels.hpp"
+
+namespace prox {
+
+// y^T = W x^T as MFMAs: 16 outputs by 16 batch rows by 32 inputs each.  The codes enter as
+// exact 16-bit values with an offset, the offset's part (bias times the sum of x, one more
+// product per 32 inputs for all NT tiles) starts each group's sum, and the scale is applied
+// to the group's fp32 sum, so that nothing is rounded before y.  Bound by HBM: the codes are read
+// once.  A workgroup takes WN * NT tiles of 16 outputs over all inputs, so that no partial
+// sums leave it; its 8 waves take NT tiles each of 8 / WN blocks of 128 inputs at a time.
+// They are added in a fixed order through LDS.
+// x goes through LDS from whole rows of 256 bytes to operand order (a load of operands
+// straight from the rows touches 64 lines at a time and takes four times as long), where the
+// WN waves of a block share it: x is read from the L2 once per workgroup, for which WN * NT
+// grows with the batch.
+// GPB: groups per block of 128 (4, 2, or 1 for groups of 128 and more).
+constexpr int kLinearWaves = 8;
+
+template <int NT, int RG, int WN>
+constexpr size_t linear_lds() {
+    constexpr int MT = (RG + 3) / 4, WK = kLinearWaves / WN, TILES = NT * MT, RT = TILES < 8 ? TILES : 8;
+    constexpr size_t stage = (WN == 1 ? 1 : 2) * (size_t)WK * MT * 4096, red = (size_t)kLinearWaves * RT * 1024;
+    return stage > red ? stage : red;
+}
+
+// RG: groups of four batch rows.
+template <int DT, int NT, int RG, int WN, int GPB, bool TAIL>
+__global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A) {
+    constexpr int MT = (RG + 3) / 4, WK = kLinearWaves / WN, TILES = NT * MT, RT = TILES < 8 ? TILES : 8;
+    static_assert(RG % WN == 0, "the waves of a block load the same number of rows");
+    constexpr int XL = RG / WN;                     // loads of 4 rows of a block by each of its waves
+    constexpr int STAGE = WK * MT * 256;            // 16-byte chunks of x: [slot][row tile][chunk of the row][row ^ chunk]
+    extern __shared__ __align__(16) unsigned char smem[];
+    u32x4 *xs = reinterpret_cast<u32x4 *>(smem);
+    const LinearLayout L(A.n, A.k, A.group);
+    const int batch = A.batch, n = A.n, k = A.k;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int lane = lane_id(), h = lane / 16, col = lane % 16;
+    const int slot = wave / WN, nw = wave % WN;
+    const int tile0 = (blockIdx.x * WN + nw) * NT;
+    const Int4Oct<DT> oct;
+    const uint4 minus = Int4Oct<DT>::minus();
+    // Load l of this wave: rows 4 (nw XL + l) + h, chunk col of 8 inputs; past the batch its
+    // last row again (their columns are not stored).
+    const uint16_t *xr[XL];
+#pragma unroll
+    for (int l = 0; l < XL; ++l) xr[l] = A.x + (size_t)min(4 * (nw * XL + l) + h, batch - 1) * A.ldx + 8 * col;
+    const uint8_t *codes[NT];
+    const uint16_t *scales[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {   // past the last tile: the last again, not stored
+        const int tile = min(tile0 + t, L.tiles - 1);
+        codes[t] = A.blob + (size_t)tile * L.blocks * 1024 + lane * 16;
+        scales[t] = reinterpret_cast<const uint16_t *>(A.blob + L.scales) + (size_t)tile * L.groups * kLinearRows + 4 * h;
+    }
+    v4f acc[NT][MT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[t][m] = v4f{0, 0, 0, 0};
+    u32x4 c[2][NT], xv[2][XL];   // of even and odd steps, two steps ahead
+    u32x2 sc[2][NT][GPB];
+    const int last = L.blocks - 1;
+    auto load_codes = [&](int b, u32x4 (&cv)[NT], u32x2 (&sv)[NT][GPB]) {   // past the end: the last block again
+        b = min(b, last);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) cv[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(codes[t] + (size_t)b * 1024));
+        const int g0 = GPB == 1 ? (int)((uint32_t)b * A.per_group >> 20) : b * GPB;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int g = 0; g < GPB; ++g)
+                sv[t][g] = *reinterpret_cast<const u32x2 *>(scales[t] + (size_t)(TAIL ? min(g0 + g, L.groups - 1) : g0 + g) * kLinearRows);
+    };
+    auto load_x = [&](int b, u32x4 (&v)[XL]) {
+        const int k0 = min(b, last) * kLinearBlock;
+        const bool in = !TAIL || k0 + 8 * col < k;
+#pragma unroll
+        for (int l = 0; l < XL; ++l) {
+            v[l] = *reinterpret_cast<const u32x4 *>(xr[l] + (TAIL && !in ? -8 * col : k0));
+            if (TAIL && !in) v[l] = u32x4{0, 0, 0, 0};
+        }
+    };
+    auto stage = [&](int buf, const u32x4 (&v)[XL]) {
+#pragma unroll
+        for (int l = 0; l < XL; ++l) {
+            const int row = 4 * (nw * XL + l) + h;
+            xs[buf * STAGE + (slot * MT + row / 16) * 256 + col * 16 + ((row % 16) ^ col)] = v[l];
+        }
+    };
+    // Step j (blocks j WK + slot) computes from its LDS buffer, asks for the codes of step
+    // j + 2, stages the x of step j + 1 and asks for that of step j + 3.
+    auto step = [&](int b, int par) {
+        const int buf = WN == 1 ? 0 : par;
+        u32x4 cc[NT];
+        u32x2 cs[NT][GPB];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            cc[t] = c[par][t];
+#pragma unroll
+            for (int g = 0; g < GPB; ++g) cs[t][g] = sc[par][t][g];
+        }
+        load_codes(b + 2 * WK, c[par], sc[par]);
+        if (b < L.blocks) {
+            const u32x4 *xb = xs + buf * STAGE + slot * MT * 256;
+#pragma unroll
+            for (int g = 0; g < GPB; ++g) {
+                v4f s[NT][MT], base[MT];
+#pragma unroll
+                for (int i = g * 4 / GPB; i < (g + 1) * 4 / GPB; ++i) {
+                    const bool first = i == g * 4 / GPB;
+                    uint4 xf[MT];
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) xf[m] = __builtin_bit_cast(uint4, xb[m * 256 + (4 * i + h) * 16 + (col ^ (4 * i + h))]);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) base[m] = mfma32<DT>(minus, xf[m], first ? v4f{0, 0, 0, 0} : base[m]);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const uint4 a = oct(cc[t][i]);
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) s[t][m] = mfma32<DT>(a, xf[m], first ? v4f{0, 0, 0, 0} : s[t][m]);
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const float f[4] = {f16_bits_to_float(cs[t][g][0] & 0xFFFFu), f16_bits_to_float(cs[t][g][0] >> 16),
+                                        f16_bits_to_float(cs[t][g][1] & 0xFFFFu), f16_bits_to_float(cs[t][g][1] >> 16)};
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[t][m][e] = fmaf(f[e], s[t][m][e] + base[m][e], acc[t][m][e]);
+                }
+            }
+        }
+        if constexpr (WN == 1) wave_lds_fence();   // x is this wave's own: LDS serves it in order
+        if (b + WK < L.blocks) stage(buf ^ (WN == 1 ? 0 : 1), xv[par ^ 1]);
+        load_x(b + 3 * WK, xv[par ^ 1]);
+        if constexpr (WN == 1) wave_lds_fence();
+        else __syncthreads();
+    };
+    load_x(slot, xv[0]);
+    load_codes(slot, c[0], sc[0]);
+    load_x(slot + WK, xv[1]);
+    load_codes(slot + WK, c[1], sc[1]);
+    if (slot < L.blocks) stage(0, xv[0]);
+    load_x(slot + 2 * WK, xv[0]);
+    if constexpr (WN == 1) wave_lds_fence();
+    else __syncthreads();
+    for (int b0 = 0; b0 < L.blocks; b0 += 2 * WK) {
+        step(b0 + slot, 0);
+        if (b0 + WK < L.blocks) step(b0 + WK + slot, 1);
+    }
+    __syncthreads();
+    // The slots' sums, RT tiles at a time, over the staging area.
+    v4f *red = reinterpret_cast<v4f *>(smem);   // [wave][RT][lane]
+#pragma unroll
+    for (int r = 0; r < TILES; r += RT) {
+        if (r > 0) __syncthreads();
+#pragma unroll
+        for (int u = 0; u < RT; ++u) red[(wave * RT + u) * kWave + lane] = acc[(r + u) / MT][(r + u) % MT];
+        __syncthreads();
+        for (int u = slot; u < RT; u += WK) {
+            v4f s = red[(nw * RT + u) * kWave + lane];
+#pragma unroll
+            for (int w = 1; w < WK; ++w) s += red[((w * WN + nw) * RT + u) * kWave + lane];
+            const int t = (r + u) / MT, b = 16 * ((r + u) % MT) + col;
+            const int j = (tile0 + t) * kLinearRows + 4 * h;
+            if (b < batch) {
+                uint16_t *dst = A.y + (size_t)b * A.ldy;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j + e < n) dst[j + e] = float_to_half<DT>(s[e] + (A.bias ? half_to_float<DT>(A.bias[j + e]) : 0.0f));
+            }
+        }
+    }
+}
+
+template <int DT, int NT, int RG, int WN, int GPB, bool TAIL>
+static hipError_t run_linear(const LinearArgs &a, hipStream_t s) {
+    constexpr int R = kLinearRows * NT * WN;
+    constexpr size_t lds = linear_lds<NT, RG, WN>();
+    auto *kernel = linear_kernel<DT, NT, RG, WN, GPB, TAIL>;
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<(unsigned)((a.n + R - 1) / R), 64 * kLinearWaves, lds, s>>>(a);
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_linear_dt(const LinearArgs &a, hipStream_t s) {
+    const int gpb = a.group == 32 ? 4 : a.group == 64 ? 2 : 1;   // a block past k has groups of 32 or 64 only
+    const bool tail = a.k % kLinearBlock != 0;
+    const int n = a.n, batch = a.batch;
+#define LINEAR(NT_, RG_, WN_)                                                                                  \
+    return (gpb == 4 ? (tail ? run_linear<DT, NT_, RG_, WN_, 4, true>(a, s) : run_linear<DT, NT_, RG_, WN_, 4, false>(a, s))                      \
+     : gpb == 2 ? (tail ? run_linear<DT, NT_, RG_, WN_, 2, true>(a, s) : run_linear<DT, NT_, RG_, WN_, 2, false>(a, s))                    \
+                : run_linear<DT, NT_, RG_, WN_, 1, false>(a, s))
+    // Outputs per workgroup (16 NT WN): the fewest of 16, 32, 64, 128 that leave at most one
+    // workgroup per CU, as each reads all of x again (in us, 32 rows, with 16 / 32 / 64 / 128:
+    // 4096 x 4096 9.1 / 10.2 / 12.7 / 18.8, 8192 x 8192 24.2 / 16.4 / 20.7 / 32.7, 14336 x 4096
+    // 28.3 / 19.4 / 13.4 / 19.5, 28672 x 8192 79.0 / 56.6 / 40.7 / 36.2).  Up to 8 rows read little
+    // of it, and 32 outputs serve every n above (28672 x 8192, one row: 26.4 / 24.8 / 27.0); up
+    // to 16 rows 64 do.  Two waves share the x of 64 rows where 16 outputs a wave would do, as
+    // it fills the registers of one (8192 x 8192, 32 outputs: 25.0, by one wave of 2 tiles 70.9).
+    const int cus = 256;
+    const int r = n <= 16 * cus ? 16 : n <= 32 * cus ? 32 : n <= 64 * cus ? 64 : 128;
+    if (batch <= 4) {
+        if (r == 16) LINEAR(1, 1, 1);
+        LINEAR(2, 1, 1);
+    }
+    if (batch <= 8) {
+        if (r == 16) LINEAR(1, 2, 1);
+        LINEAR(2, 2, 1);
+    }
+    if (batch <= 16) {
+        if (r == 16) LINEAR(1, 4, 1);
+        if (r == 32) LINEAR(2, 4, 1);
+        LINEAR(4, 4, 1);
+    }
+    if (batch <= 32) {
+        if (r == 16) LINEAR(1, 8, 1);
+        if (r == 32) LINEAR(2, 8, 1);
+        if (r == 64) LINEAR(2, 8, 2);
+        LINEAR(2, 8, 4);
+    }
+    if (r <= 32) LINEAR(1, 16, 2);
+    if (r == 64) LINEAR(2, 16, 2);
+    LINEAR(2, 16, 4);
+#undef LINEAR
+}
+
+}  // namespace prox
