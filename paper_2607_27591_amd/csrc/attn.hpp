@@ -1,0 +1,440 @@
+// Attention of new tokens over the 4-bit paged cache: the kernels, and their variant by shape.
+// Compiled once per dtype (attn_f16.hip, attn_bf16.hip).
+#pragma once
+
+#include "common.hpp"
+#include "kernels.hpp"
+
+namespace prox {
+
+constexpr int kAttnWaves = 4;
+constexpr int kAttnMinBlocks = 4;      // blocks of 32 tokens per workgroup, before the cache is split
+constexpr float kAttnNone = -3.0e38f;  // running maximum before the first score (finite: no inf - inf)
+// The running maximum m of a row's scores (log2) is raised only when a score exceeds it by more
+// than this: weights stay below 2^8, and sums and outputs are rescaled a few times in all.
+constexpr float kAttnSlack = 8.0f;
+
+// Blocks that a tile of query rows sees, and how they are split: split k takes blocks
+// [b0 + k per, b0 + (k + 1) per) of [b0, b1); eff splits have any.  Row r of a sequence and kv
+// head is new token r / ratio, query head r % ratio of the kv head.
+struct AttnSpan {
+    int b0, b1, per, eff;
+};
+__device__ __forceinline__ AttnSpan attn_span(const AttnArgs &A, const SeqTokens &q, int r0, int r1) {
+    const int hi = q.pos0 + r1 / A.ratio, lo = A.window > 0 ? max(q.pos0 + r0 / A.ratio - A.window + 1, 0) : 0;
+    if (hi < 0) return AttnSpan{0, 0, 1, 0};
+    AttnSpan s;
+    s.b0 = lo / kKvBlock;
+    s.b1 = hi / kKvBlock + 1;
+    s.per = max((s.b1 - s.b0 + A.splits - 1) / A.splits, kAttnMinBlocks);
+    s.eff = (s.b1 - s.b0 + s.per - 1) / s.per;
+    return s;
+}
+
+template <int W>
+__device__ __forceinline__ void load_words(uint32_t (&out)[W], const uint8_t *p) {
+    if constexpr (W == 2) {
+        const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p));
+        out[0] = v[0];
+        out[1] = v[1];
+    } else {
+#pragma unroll
+        for (int i = 0; i < W / 4; ++i) {
+            const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p) + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[4 * i + e] = v[e];
+        }
+    }
+}
+
+// Scale of token 4 h + e of half block j (kv_slot: 16 h + .. are this lane's 8 in a row).
+__device__ __forceinline__ float slot_scale(const u32x4 &v, int j, int e) {
+    const uint32_t w = v[2 * j + e / 2];
+    return f16_bits_to_float((e & 1) ? w >> 16 : w & 0xFFFFu);
+}
+
+typedef __bf16 bf16v2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {   // rounded to nearest even
+    const bf16v2 v = {(__bf16)lo, (__bf16)hi};
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+__device__ __forceinline__ float max_swap16(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_swap32(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Row `row` of the partial results: head_dim sums, then (maximum, sum of weights) of all rows.
+__device__ __forceinline__ size_t attn_part_row(const AttnArgs &A, int split, int s, int head, int tile, int R) {
+    return ((((size_t)split * A.s.n_seq + s) * A.c.heads + head) * A.tiles + tile) * R;
+}
+
+// One pass over the cache with the running maximum and sum of the softmax.  A wave takes
+// blocks of 32 tokens; with K the codes of 16 tokens and Q 16 query rows of one kv head,
+//   S^T = K Q^T             codes exact with an offset (base starts each group's sum), scales
+//                           on the fp32 sums: lane l gets tokens 4 (l / 16) + e of row l % 16
+//   P   = 2^(c S - m)       fp32; l += P
+//   O^T += V^T (P sv)^T     P times the values' scale, rounded to two bf16 terms (2^-17), is
+//                           the second product's operand as it stands, no lane exchange; the
+//                           codes' offset comes off with a product of its own (acc_off), before
+//                           it can outgrow the sums (every 8 blocks).
+// Two terms, as one bf16 term would add as much error as the rounding of a bf16 output, and
+// eight times that of an fp16 one; bf16 and not fp16, as P sv spans any range.
+// Bound by HBM for single tokens (a record is read once and contiguous; the next one's loads
+// are in flight), by VALU issue for many rows, for which QT tiles of 16 rows share the codes.
+// The four waves' results are joined through LDS, those of several workgroups of a long
+// cache by attn_join_kernel.
+template <int DT, int D, int NG, int QT>
+__global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
+    constexpr int R = 16 * QT, KW = D / 32, VT = D / 16, SPG = KW / NG, VPG = VT / NG;
+    constexpr int TC = VT < 8 ? VT : 8;   // channel tiles joined at a time
+    constexpr KvLayout L(D, D / NG);
+    __shared__ v4f o_sh[kAttnWaves][TC][kWave];
+    __shared__ float m_sh[kAttnWaves][16], l_sh[kAttnWaves][16];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int lane = lane_id(), h = lane / 16, col = lane % 16;
+    int id = blockIdx.x;
+    const int split = id % A.splits;
+    id /= A.splits;
+    const int tile = id % A.tiles;
+    id /= A.tiles;
+    const int head = id % A.c.heads, s = id / A.c.heads;
+    const SeqTokens sq = seq_tokens(A.s, s);
+    const int rows = sq.n * A.ratio, r0 = tile * R;
+    if (r0 >= rows) return;
+    const AttnSpan sp = attn_span(A, sq, r0, min(r0 + R, rows) - 1);
+    if (split > 0 && split >= sp.eff) return;
+    const int b_end = min(sp.b0 + (split + 1) * sp.per, sp.b1);
+
+    // Queries as operands, and what each lane's row may see.
+    uint4 q[QT][KW];
+    int lo[QT], hi[QT];
+    int lo_max = 0, hi_min = 0x7FFFFFFF;
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        const int r = min(r0 + 16 * u + col, rows - 1), i = r / A.ratio;   // past the last row: it again
+        const uint16_t *p = A.q + (size_t)(sq.t0 + i) * A.ldq + (size_t)(head * A.ratio + r - i * A.ratio) * D + 8 * h;
+#pragma unroll
+        for (int w = 0; w < KW; ++w) q[u][w] = *reinterpret_cast<const uint4 *>(p + 32 * w);
+        hi[u] = sq.pos0 + i;
+        lo[u] = A.window > 0 ? hi[u] - A.window + 1 : 0;
+    }
+    {   // over the tile's rows, from its first and last
+        const int i0 = r0 / A.ratio, i1 = (min(r0 + R, rows) - 1) / A.ratio;
+        hi_min = sq.pos0 + i0;
+        lo_max = A.window > 0 ? sq.pos0 + i1 - A.window + 1 : 0;
+    }
+    const int hi_max = sq.pos0 + (min(r0 + R, rows) - 1) / A.ratio;
+    const int lo_min = A.window > 0 ? hi_min - A.window + 1 : 0;
+
+    const Int4Oct<DT> kop;
+    const Int4Oct<kBF16> vop;
+    const uint4 kminus = Int4Oct<DT>::minus(), vminus = Int4Oct<kBF16>::minus();
+    const v4f zero{0, 0, 0, 0};
+    v4f base[QT][NG];
+#pragma unroll
+    for (int u = 0; u < QT; ++u)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            base[u][g] = zero;
+#pragma unroll
+            for (int w = g * SPG; w < (g + 1) * SPG; ++w) base[u][g] = mfma32<DT>(kminus, q[u][w], base[u][g]);
+        }
+    v4f acc[QT][VT], acc_off[QT][NG];
+    float m[QT], l[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        m[u] = kAttnNone;
+        l[u] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VT; ++i) acc[u][i] = zero;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) acc_off[u][g] = zero;
+    }
+
+    struct Block {
+        uint32_t k[2][KW], v[VT];
+        u32x4 ks[NG], vs[NG];
+    };
+    const int32_t *table = A.s.table + (size_t)s * A.s.max_pages;
+    const int per = A.c.page_size / kKvBlock;
+    auto load = [&](int b, Block &x) -> bool {   // false: the page lies outside the cache
+        b = min(b, sp.b1 - 1);
+        const int page = A.page_shift >= 0 ? b >> A.page_shift : b / per;
+        const int pid = __builtin_amdgcn_readfirstlane(table[page]);
+        const bool ok = pid >= 0 && pid < A.c.n_pages;
+        if (ok) {
+            const uint8_t *rec = A.c.blob + (size_t)pid * A.c.page_bytes + ((size_t)head * per + (b - page * per)) * L.record;
+            load_words(x.k[0], rec + lane * (KW * 4));
+            load_words(x.k[1], rec + (64 + lane) * (KW * 4));
+            load_words(x.v, rec + L.v_codes + lane * (VT * 4));
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                x.ks[g] = *reinterpret_cast<const u32x4 *>(rec + L.k_scales + g * 64 + h * 16);
+                x.vs[g] = *reinterpret_cast<const u32x4 *>(rec + L.v_scales + g * 64 + h * 16);
+            }
+        }
+        return ok;
+    };
+    auto flush = [&] {
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+#pragma unroll
+                for (int i = g * VPG; i < (g + 1) * VPG; ++i) acc[u][i] += acc_off[u][g];
+                acc_off[u][g] = zero;
+            }
+    };
+    Block nx;
+    bool nx_ok = false;
+    const int first = sp.b0 + split * sp.per + wave;
+    if (first < b_end) nx_ok = load(first, nx);
+    int done = 0;
+    for (int b = first; b < b_end; b += kAttnWaves) {
+        const Block x = nx;
+        const bool ok = nx_ok;
+        if (b + kAttnWaves < b_end) nx_ok = load(b + kAttnWaves, nx);
+        if (!ok) continue;
+        float sc[QT][2][4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                v4f d[QT];
+#pragma unroll
+                for (int w = g * SPG; w < (g + 1) * SPG; ++w) {
+                    const uint4 a = kop(x.k[j][w]);
+#pragma unroll
+                    for (int u = 0; u < QT; ++u) d[u] = mfma32<DT>(a, q[u][w], w == g * SPG ? base[u][g] : d[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < QT; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float f = slot_scale(x.ks[g], j, e);
+                        sc[u][j][e] = g == 0 ? d[u][e] * f : fmaf(d[u][e], f, sc[u][j][e]);
+                    }
+            }
+        }
+        const int p0 = b * kKvBlock;
+        const bool edge = p0 + kKvBlock - 1 > hi_min || p0 < lo_max;   // some row does not see all of it
+        bool up = false;
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            float mx = kAttnNone;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float v = sc[u][j][e] * A.scale;
+                    if (edge) {
+                        const int p = p0 + 16 * j + 4 * h + e;
+                        v = p <= hi[u] && p >= lo[u] ? v : -INFINITY;   // whatever stands there
+                    }
+                    sc[u][j][e] = v;
+                    mx = fmaxf(mx, v);
+                }
+            up |= mx > m[u] + kAttnSlack;
+        }
+        if (__any(up)) {
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                float mx = m[u];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[u][j][e]);
+                mx = max_swap32(max_swap16(mx));
+                const float f = __builtin_amdgcn_exp2f(m[u] - mx);
+                m[u] = mx;
+                l[u] *= f;
+#pragma unroll
+                for (int i = 0; i < VT; ++i) acc[u][i] *= f;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) acc_off[u][g] *= f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sc[u][j][e] = __builtin_amdgcn_exp2f(sc[u][j][e] - m[u]);
+                    l[u] += sc[u][j][e];
+                }
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            uint4 ph[QT], pl[QT];
+            float f[2][4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    f[j][e] = slot_scale(x.vs[g], j, e);
+                    if (edge) {   // tokens that no row sees may hold anything
+                        const int p = p0 + 16 * j + 4 * h + e;
+                        f[j][e] = p <= hi_max && p >= lo_min ? f[j][e] : 0.0f;
+                    }
+                }
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                uint32_t wh[4], wl[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = sc[u][0][e] * f[0][e], c = sc[u][1][e] * f[1][e];
+                    wh[e] = pack_bf16(a, c);
+                    wl[e] = pack_bf16(a - bf16_lo(wh[e]), c - bf16_hi(wh[e]));
+                }
+                ph[u] = make_uint4(wh[0], wh[1], wh[2], wh[3]);
+                pl[u] = make_uint4(wl[0], wl[1], wl[2], wl[3]);
+                acc_off[u][g] = mfma32<kBF16>(vminus, ph[u], acc_off[u][g]);
+                acc_off[u][g] = mfma32<kBF16>(vminus, pl[u], acc_off[u][g]);
+            }
+#pragma unroll
+            for (int i = g * VPG; i < (g + 1) * VPG; ++i) {
+                const uint4 a = vop(x.v[i]);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) acc[u][i] = mfma32<kBF16>(a, ph[u], acc[u][i]);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) acc[u][i] = mfma32<kBF16>(a, pl[u], acc[u][i]);
+            }
+        }
+        if ((++done & 7) == 0) flush();
+    }
+    flush();
+
+    // The waves' results: o = sum_w 2^(m_w - m) o_w, l alike, in a fixed order.
+    float *part_o = reinterpret_cast<float *>(A.ws);
+    float2 *part_ml = reinterpret_cast<float2 *>(part_o + (size_t)kAttnPartRows * D);
+    const size_t prow = attn_part_row(A, split, s, head, tile, R);
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        const float lw = add_swap32(add_swap16(l[u]));
+        if (u > 0) __syncthreads();
+        if (h == 0) {
+            m_sh[wave][col] = m[u];
+            l_sh[wave][col] = lw;
+        }
+        __syncthreads();
+        float mm = m_sh[0][col], ll = 0.0f;
+#pragma unroll
+        for (int w = 1; w < kAttnWaves; ++w) mm = fmaxf(mm, m_sh[w][col]);
+#pragma unroll
+        for (int w = 0; w < kAttnWaves; ++w) ll = fmaf(l_sh[w][col], __builtin_amdgcn_exp2f(m_sh[w][col] - mm), ll);
+        const float f = __builtin_amdgcn_exp2f(m[u] - mm);
+        const int r = r0 + 16 * u + col, i = r / A.ratio;
+        uint16_t *dst = A.out + (size_t)(sq.t0 + i) * A.ldo + (size_t)(head * A.ratio + r - i * A.ratio) * D + 4 * h;
+        const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+        if (sp.eff > 1 && wave == 0 && h == 0 && r < rows) part_ml[prow + 16 * u + col] = make_float2(mm, ll);
+#pragma unroll
+        for (int c = 0; c < VT; c += TC) {
+            if (c > 0) __syncthreads();
+#pragma unroll
+            for (int i2 = 0; i2 < TC; ++i2) o_sh[wave][i2][lane] = acc[u][c + i2] * f;
+            __syncthreads();
+            for (int i2 = wave; i2 < TC; i2 += kAttnWaves) {
+                v4f o = o_sh[0][i2][lane];
+#pragma unroll
+                for (int w = 1; w < kAttnWaves; ++w) o += o_sh[w][i2][lane];
+                if (r >= rows) continue;
+                if (sp.eff > 1) {
+                    *reinterpret_cast<v4f *>(part_o + (prow + 16 * u + col) * D + 16 * (c + i2) + 4 * h) = o;
+                } else {
+                    const uint32_t w0 = float_to_half<DT>(o[0] * inv) | (uint32_t)float_to_half<DT>(o[1] * inv) << 16;
+                    const uint32_t w1 = float_to_half<DT>(o[2] * inv) | (uint32_t)float_to_half<DT>(o[3] * inv) << 16;
+                    *reinterpret_cast<uint2 *>(dst + 16 * (c + i2)) = make_uint2(w0, w1);
+                }
+            }
+        }
+    }
+}
+
+// The splits' results of one query row per wave, in a fixed order.
+template <int DT, int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A, int R) {
+    constexpr int PL = D / kWave;
+    const int lane = lane_id();
+    const long long row = (long long)blockIdx.x * 4 + threadIdx.x / kWave;   // (sequence, new token, query head)
+    if (row >= (long long)A.s.n_seq * A.s.max_new * A.q_heads) return;
+    const int hq = (int)(row % A.q_heads), s = (int)(row / A.q_heads / A.s.max_new), i = (int)(row / A.q_heads % A.s.max_new);
+    const SeqTokens sq = seq_tokens(A.s, s);
+    if (i >= sq.n) return;
+    const int head = hq / A.ratio, r = i * A.ratio + hq % A.ratio, tile = r / R;
+    const AttnSpan sp = attn_span(A, sq, tile * R, min((tile + 1) * R, sq.n * A.ratio) - 1);
+    if (sp.eff <= 1) return;
+    const float *part_o = reinterpret_cast<const float *>(A.ws);
+    const float2 *part_ml = reinterpret_cast<const float2 *>(part_o + (size_t)kAttnPartRows * D);
+    const size_t stride = attn_part_row(A, 1, 0, 0, 0, R), at = attn_part_row(A, 0, s, head, tile, R) + r % R;
+    float mm = kAttnNone;
+    for (int k = lane; k < sp.eff; k += kWave) mm = fmaxf(mm, part_ml[at + k * stride].x);
+    for (int x = 1; x < kWave; x <<= 1) mm = fmaxf(mm, __shfl_xor(mm, x));
+    float ll = 0.0f, o[PL] = {};
+    for (int k0 = 0; k0 < sp.eff; k0 += kWave) {
+        float f = 0.0f;
+        if (k0 + lane < sp.eff) {
+            const float2 ml = part_ml[at + (k0 + lane) * stride];
+            f = __builtin_amdgcn_exp2f(ml.x - mm);
+            ll = fmaf(ml.y, f, ll);
+        }
+        const int n = min(sp.eff - k0, kWave);
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) {
+            const float w = __shfl(f, k);
+            const float *src = part_o + (at + (size_t)(k0 + k) * stride) * D + lane * PL;
+#pragma unroll
+            for (int e = 0; e < PL; ++e) o[e] = fmaf(w, src[e], o[e]);
+        }
+    }
+    ll = wave_sum(ll);
+    const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+    uint16_t *dst = A.out + (size_t)(sq.t0 + i) * A.ldo + (size_t)hq * D + lane * PL;
+#pragma unroll
+    for (int e = 0; e < PL; ++e) dst[e] = float_to_half<DT>(o[e] * inv);
+}
+
+template <int DT, int D, int NG, int QT>
+hipError_t run_attn(AttnArgs &a, hipStream_t s) {
+    constexpr int R = 16 * QT;
+    a.tiles = (int)(((long long)a.s.max_new * a.ratio + R - 1) / R);
+    // Splits: enough workgroups of four waves to keep several on each CU, as far as the
+    // partial results fit their area.
+    const long long base = (long long)a.s.n_seq * a.c.heads * a.tiles;
+    const int blocks = (a.s.max_kv + kKvBlock - 1) / kKvBlock;
+    long long n = base >= 1024 ? 1 : 1024 / base;
+    if (n > kAttnPartRows / R / base) n = kAttnPartRows / R / base;
+    if (n > (blocks + kAttnMinBlocks - 1) / kAttnMinBlocks) n = (blocks + kAttnMinBlocks - 1) / kAttnMinBlocks;
+    a.splits = n < 1 ? 1 : (int)n;
+    attn_kernel<DT, D, NG, QT><<<(unsigned)(base * a.splits), 64 * kAttnWaves, 0, s>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    const long long rows = (long long)a.s.n_seq * a.s.max_new * a.q_heads;
+    attn_join_kernel<DT, D><<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(a, R);
+    return hipGetLastError();
+}
+
+template <int DT, int D, int NG>
+hipError_t launch_attn_rows(AttnArgs &a, hipStream_t s) {
+    const long long rows = (long long)a.s.max_new * a.ratio;
+    if (rows <= 16) return run_attn<DT, D, NG, 1>(a, s);
+    if (rows <= 32 || D == 256) return run_attn<DT, D, NG, 2>(a, s);
+    return run_attn<DT, D, NG, D == 256 ? 2 : 4>(a, s);
+}
+
+template <int DT>
+hipError_t launch_attn_dt(AttnArgs &a, hipStream_t s) {
+    const int ng = a.c.dim / a.c.group;
+    if (a.c.dim == 64) return ng == 1 ? launch_attn_rows<DT, 64, 1>(a, s) : launch_attn_rows<DT, 64, 2>(a, s);
+    if (a.c.dim == 128)
+        return ng == 1 ? launch_attn_rows<DT, 128, 1>(a, s)
+               : ng == 2 ? launch_attn_rows<DT, 128, 2>(a, s) : launch_attn_rows<DT, 128, 4>(a, s);
+    return ng == 2 ? launch_attn_rows<DT, 256, 2>(a, s)
+           : ng == 4 ? launch_attn_rows<DT, 256, 4>(a, s) : launch_attn_rows<DT, 256, 8>(a, s);
+}
+
+}  // namespace prox

@@ -153,8 +153,19 @@ hipError_t launch_kv_append(int dtype, const KvCache &c, const KvSeqs &s, const 
                             const void *v, int64_t ldv, const void *q, int q_heads, int64_t ldq,
                             void *q_out, int64_t ldq_out, const Rope &rope, hipStream_t stream);
 hipError_t launch_kv_read(const KvCache &c, const KvSeqs &s, float *k, float *v, hipStream_t stream);
-hipError_t launch_attn(int dtype, const KvCache &c, const KvSeqs &s, const void *q, int q_heads,
-                       int64_t ldq, float scale, int window, void *out, int64_t ldo, void *ws,
-                       hipStream_t stream);
+struct AttnArgs {
+    KvCache c;
+    KvSeqs s;
+    const uint16_t *q;
+    uint16_t *out;
+    int64_t ldq, ldo;
+    int q_heads, ratio, window;   // ratio: query heads per kv head
+    float scale;                  // times log2 e
+    int page_shift;               // log2 of the blocks of a page, or -1
+    void *ws;
+    int tiles, splits;            // set by the launch
+};
+hipError_t launch_attn_bf16(AttnArgs &a, hipStream_t stream);
+hipError_t launch_attn_f16(AttnArgs &a, hipStream_t stream);
 
 }  // namespace prox
