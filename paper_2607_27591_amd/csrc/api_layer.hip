@@ -167,7 +167,8 @@ prox_status prox_kv_attn(const prox_kv_cache *c, const prox_kv_seqs *s, const vo
     if ((long long)ks.n_seq * ks.max_new * q_heads > kMaxGrid) return PROX_ERR_UNSUPPORTED;
     const int per = kc.page_size / kKvBlock;
     AttnArgs a{kc, ks, static_cast<const uint16_t *>(q), static_cast<uint16_t *>(out), ldq, ldo, q_heads,
-               q_heads / kc.heads, window, (float)((double)scale * 1.4426950408889634), -1, ws, 0, 0};
+               q_heads / kc.heads, window, (float)(std::fabs((double)scale) * 1.4426950408889634),
+               scale < 0 ? 0x80008000u : 0u, -1, ws, 0, 0, 0};
     for (int i = 0; i < 16; ++i)
         if (per == 1 << i) a.page_shift = i;
     return hip_status(c->dtype == PROX_BF16 ? launch_attn_bf16(a, stream) : launch_attn_f16(a, stream));

@@ -1,6 +1,7 @@
 // Attention of new tokens over the 4-bit paged cache: the kernels, and their variant by shape.
 // Compiled once per dtype (attn_f16.hip, attn_bf16.hip).
 #pragma once
+#include <cstdlib>
 
 #include "common.hpp"
 #include "kernels.hpp"
@@ -31,6 +32,9 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs &A, const SeqTokens
     return s;
 }
 
+// Waves per SIMD that the registers are to allow.
+constexpr int attn_waves(int D, int NG, int QT) { return QT == 1 ? (D == 256 ? 2 : D == 128 ? 3 : 4) : QT == 2 && D <= 128 ? 2 : 1; }
+
 template <int W>
 __device__ __forceinline__ void load_words(uint32_t (&out)[W], const uint8_t *p) {
     if constexpr (W == 2) {
@@ -53,11 +57,24 @@ __device__ __forceinline__ float slot_scale(const u32x4 &v, int j, int e) {
     return f16_bits_to_float((e & 1) ? w >> 16 : w & 0xFFFFu);
 }
 
+// a * s with s an fp16 scale in place: as a fused add of 0 it is one v_fma_mix_f32, without a
+// conversion (a and s nonnegative, or the result added up: the sign of a zero is no matter).
+__device__ __forceinline__ float times(float a, float s) { return fmaf(a, s, 0.0f); }
+
 typedef __bf16 bf16v2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {   // rounded to nearest even
     const bf16v2 v = {(__bf16)lo, (__bf16)hi};
     return __builtin_bit_cast(uint32_t, v);
 }
+// a - lo(w) and a - hi(w), what a rounding to bf16 left over (exact): one dot product each,
+// with (-1, 0) and (0, -1).  The constants stay in registers: as literals the compiler
+// encodes them wrongly.
+struct Bf16Left {
+    uint32_t lo = 0x0000BF80u, hi = 0xBF800000u;
+    __device__ __forceinline__ Bf16Left() { asm("" : "+v"(lo), "+v"(hi)); }
+    __device__ __forceinline__ float minus_lo(float a, uint32_t w) const { return dot2<kBF16>(w, lo, a); }
+    __device__ __forceinline__ float minus_hi(float a, uint32_t w) const { return dot2<kBF16>(w, hi, a); }
+};
 
 __device__ __forceinline__ float max_swap16(float v) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -68,9 +85,10 @@ __device__ __forceinline__ float max_swap32(float v) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// Row `row` of the partial results: head_dim sums, then (maximum, sum of weights) of all rows.
-__device__ __forceinline__ size_t attn_part_row(const AttnArgs &A, int split, int s, int head, int tile, int R) {
-    return ((((size_t)split * A.s.n_seq + s) * A.c.heads + head) * A.tiles + tile) * R;
+// First row of the partial results of a tile: head_dim sums a row, then (maximum, sum of
+// weights) of all rows.
+__device__ __forceinline__ size_t attn_part_row(const AttnArgs &A, int split, int s, int head, int tile) {
+    return ((((size_t)split * A.s.n_seq + s) * A.c.heads + head) * A.tiles + tile) * A.part_rows;
 }
 
 // One pass over the cache with the running maximum and sum of the softmax.  A wave takes
@@ -89,7 +107,7 @@ __device__ __forceinline__ size_t attn_part_row(const AttnArgs &A, int split, in
 // The four waves' results are joined through LDS, those of several workgroups of a long
 // cache by attn_join_kernel.
 template <int DT, int D, int NG, int QT>
-__global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
+__global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_kernel(AttnArgs A) {
     constexpr int R = 16 * QT, KW = D / 32, VT = D / 16, SPG = KW / NG, VPG = VT / NG;
     constexpr int TC = VT < 8 ? VT : 8;   // channel tiles joined at a time
     constexpr KvLayout L(D, D / NG);
@@ -110,6 +128,43 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
     if (split > 0 && split >= sp.eff) return;
     const int b_end = min(sp.b0 + (split + 1) * sp.per, sp.b1);
 
+    uint32_t xk[2][KW], xv[VT];
+    u32x4 xks[NG], xvs[NG];
+    const int32_t *table = A.s.table + (size_t)s * A.s.max_pages;
+    const int per = A.c.page_size / kKvBlock;
+    auto page_of = [&](int b) { return A.page_shift >= 0 ? b >> A.page_shift : b / per; };
+    auto page_id = [&](int b) { return table[page_of(min(b, sp.b1 - 1))]; };
+    // Record of block b; where its page lies outside the cache, or past the end, ok is false
+    // and the cache's first record stands in (loaded, not used).
+    auto record = [&](int b, int id, bool &ok) {
+        const int pid = __builtin_amdgcn_readfirstlane(id);
+        ok = b < b_end && pid >= 0 && pid < A.c.n_pages;
+        const size_t at = (size_t)pid * A.c.page_bytes + ((size_t)head * per + (b - page_of(b) * per)) * L.record;
+        return A.c.blob + (ok ? at : 0);
+    };
+    auto load_k = [&](const uint8_t *rec) {
+        load_words(xk[0], rec + lane * (KW * 4));
+        load_words(xk[1], rec + (64 + lane) * (KW * 4));
+#pragma unroll
+        for (int g = 0; g < NG; ++g) xks[g] = *reinterpret_cast<const u32x4 *>(rec + L.k_scales + g * 64 + h * 16);
+    };
+    auto load_v = [&](const uint8_t *rec) {
+        load_words(xv, rec + L.v_codes + lane * (VT * 4));
+#pragma unroll
+        for (int g = 0; g < NG; ++g) xvs[g] = *reinterpret_cast<const u32x4 *>(rec + L.v_scales + g * 64 + h * 16);
+    };
+    // Keys of the next block are asked for once this block's are used, values likewise; the
+    // page of the one after it.
+    const int first = sp.b0 + split * sp.per + wave;
+    int next_id = 0;
+    bool next_ok = false;
+    const uint8_t *next = A.c.blob;
+    if (first < b_end) {
+        next = record(first, page_id(first), next_ok);
+        next_id = page_id(first + kAttnWaves);
+        load_k(next);
+        load_v(next);
+    }
     // Queries as operands, and what each lane's row may see.
     uint4 q[QT][KW];
     int lo[QT], hi[QT];
@@ -119,7 +174,13 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
         const int r = min(r0 + 16 * u + col, rows - 1), i = r / A.ratio;   // past the last row: it again
         const uint16_t *p = A.q + (size_t)(sq.t0 + i) * A.ldq + (size_t)(head * A.ratio + r - i * A.ratio) * D + 8 * h;
 #pragma unroll
-        for (int w = 0; w < KW; ++w) q[u][w] = *reinterpret_cast<const uint4 *>(p + 32 * w);
+        for (int w = 0; w < KW; ++w) {
+            q[u][w] = *reinterpret_cast<const uint4 *>(p + 32 * w);
+            q[u][w].x ^= A.q_sign;
+            q[u][w].y ^= A.q_sign;
+            q[u][w].z ^= A.q_sign;
+            q[u][w].w ^= A.q_sign;
+        }
         hi[u] = sq.pos0 + i;
         lo[u] = A.window > 0 ? hi[u] - A.window + 1 : 0;
     }
@@ -133,6 +194,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
 
     const Int4Oct<DT> kop;
     const Int4Oct<kBF16> vop;
+    const Bf16Left left;
     const uint4 kminus = Int4Oct<DT>::minus(), vminus = Int4Oct<kBF16>::minus();
     const v4f zero{0, 0, 0, 0};
     v4f base[QT][NG];
@@ -145,10 +207,12 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
             for (int w = g * SPG; w < (g + 1) * SPG; ++w) base[u][g] = mfma32<DT>(kminus, q[u][w], base[u][g]);
         }
     v4f acc[QT][VT], acc_off[QT][NG];
-    float m[QT], l[QT];
+    // Running maximum m of scale times the score; a score above top raises it.
+    float m[QT], l[QT], top[QT];
+    const float slack = kAttnSlack / A.scale;
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
-        m[u] = kAttnNone;
+        m[u] = top[u] = kAttnNone;
         l[u] = 0.0f;
 #pragma unroll
         for (int i = 0; i < VT; ++i) acc[u][i] = zero;
@@ -156,30 +220,6 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
         for (int g = 0; g < NG; ++g) acc_off[u][g] = zero;
     }
 
-    struct Block {
-        uint32_t k[2][KW], v[VT];
-        u32x4 ks[NG], vs[NG];
-    };
-    const int32_t *table = A.s.table + (size_t)s * A.s.max_pages;
-    const int per = A.c.page_size / kKvBlock;
-    auto load = [&](int b, Block &x) -> bool {   // false: the page lies outside the cache
-        b = min(b, sp.b1 - 1);
-        const int page = A.page_shift >= 0 ? b >> A.page_shift : b / per;
-        const int pid = __builtin_amdgcn_readfirstlane(table[page]);
-        const bool ok = pid >= 0 && pid < A.c.n_pages;
-        if (ok) {
-            const uint8_t *rec = A.c.blob + (size_t)pid * A.c.page_bytes + ((size_t)head * per + (b - page * per)) * L.record;
-            load_words(x.k[0], rec + lane * (KW * 4));
-            load_words(x.k[1], rec + (64 + lane) * (KW * 4));
-            load_words(x.v, rec + L.v_codes + lane * (VT * 4));
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                x.ks[g] = *reinterpret_cast<const u32x4 *>(rec + L.k_scales + g * 64 + h * 16);
-                x.vs[g] = *reinterpret_cast<const u32x4 *>(rec + L.v_scales + g * 64 + h * 16);
-            }
-        }
-        return ok;
-    };
     auto flush = [&] {
 #pragma unroll
         for (int u = 0; u < QT; ++u)
@@ -190,17 +230,13 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
                 acc_off[u][g] = zero;
             }
     };
-    Block nx;
-    bool nx_ok = false;
-    const int first = sp.b0 + split * sp.per + wave;
-    if (first < b_end) nx_ok = load(first, nx);
     int done = 0;
     for (int b = first; b < b_end; b += kAttnWaves) {
-        const Block x = nx;
-        const bool ok = nx_ok;
-        if (b + kAttnWaves < b_end) nx_ok = load(b + kAttnWaves, nx);
-        if (!ok) continue;
+        const bool ok = next_ok;
+        next = record(b + kAttnWaves, next_id, next_ok);
+        next_id = page_id(b + 2 * kAttnWaves);
         float sc[QT][2][4];
+        if (ok) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
@@ -208,7 +244,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
                 v4f d[QT];
 #pragma unroll
                 for (int w = g * SPG; w < (g + 1) * SPG; ++w) {
-                    const uint4 a = kop(x.k[j][w]);
+                    const uint4 a = kop(xk[j][w]);
 #pragma unroll
                     for (int u = 0; u < QT; ++u) d[u] = mfma32<DT>(a, q[u][w], w == g * SPG ? base[u][g] : d[u]);
                 }
@@ -216,42 +252,51 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
                 for (int u = 0; u < QT; ++u)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float f = slot_scale(x.ks[g], j, e);
-                        sc[u][j][e] = g == 0 ? d[u][e] * f : fmaf(d[u][e], f, sc[u][j][e]);
+                        const float f = slot_scale(xks[g], j, e);
+                        sc[u][j][e] = g == 0 ? times(d[u][e], f) : fmaf(d[u][e], f, sc[u][j][e]);
                     }
             }
         }
+        }
+        load_k(next);
+        if (ok) {
         const int p0 = b * kKvBlock;
         const bool edge = p0 + kKvBlock - 1 > hi_min || p0 < lo_max;   // some row does not see all of it
+        uint32_t seen[QT];   // bit 4 j + e: the row sees the token
         bool up = false;
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
             float mx = kAttnNone;
+            if (edge) {
+                seen[u] = 0;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int p = p0 + 16 * j + 4 * h + e;
+                        const bool ok2 = p <= hi[u] && p >= lo[u];
+                        seen[u] |= (uint32_t)ok2 << (4 * j + e);
+                        sc[u][j][e] = ok2 ? sc[u][j][e] : kAttnNone;   // whatever stands there
+                    }
+            }
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float v = sc[u][j][e] * A.scale;
-                    if (edge) {
-                        const int p = p0 + 16 * j + 4 * h + e;
-                        v = p <= hi[u] && p >= lo[u] ? v : -INFINITY;   // whatever stands there
-                    }
-                    sc[u][j][e] = v;
-                    mx = fmaxf(mx, v);
-                }
-            up |= mx > m[u] + kAttnSlack;
+                for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[u][j][e]);
+            up |= mx > top[u];
         }
         if (__any(up)) {
 #pragma unroll
             for (int u = 0; u < QT; ++u) {
-                float mx = m[u];
+                float mx = kAttnNone;
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[u][j][e]);
                 mx = max_swap32(max_swap16(mx));
-                const float f = __builtin_amdgcn_exp2f(m[u] - mx);
-                m[u] = mx;
+                const float m2 = fmaxf(m[u], mx * A.scale), f = __builtin_amdgcn_exp2f(m[u] - m2);
+                top[u] = fmaxf(top[u], mx + slack);
+                m[u] = m2;
                 l[u] *= f;
 #pragma unroll
                 for (int i = 0; i < VT; ++i) acc[u][i] *= f;
@@ -265,8 +310,10 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    sc[u][j][e] = __builtin_amdgcn_exp2f(sc[u][j][e] - m[u]);
-                    l[u] += sc[u][j][e];
+                    float p = __builtin_amdgcn_exp2f(fmaf(sc[u][j][e], A.scale, -m[u]));
+                    if (edge) p = (seen[u] >> (4 * j + e)) & 1 ? p : 0.0f;
+                    sc[u][j][e] = p;
+                    l[u] += p;
                 }
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
@@ -276,7 +323,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    f[j][e] = slot_scale(x.vs[g], j, e);
+                    f[j][e] = slot_scale(xvs[g], j, e);
                     if (edge) {   // tokens that no row sees may hold anything
                         const int p = p0 + 16 * j + 4 * h + e;
                         f[j][e] = p <= hi_max && p >= lo_min ? f[j][e] : 0.0f;
@@ -287,9 +334,9 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
                 uint32_t wh[4], wl[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float a = sc[u][0][e] * f[0][e], c = sc[u][1][e] * f[1][e];
+                    const float a = times(sc[u][0][e], f[0][e]), c = times(sc[u][1][e], f[1][e]);
                     wh[e] = pack_bf16(a, c);
-                    wl[e] = pack_bf16(a - bf16_lo(wh[e]), c - bf16_hi(wh[e]));
+                    wl[e] = pack_bf16(left.minus_lo(a, wh[e]), left.minus_hi(c, wh[e]));
                 }
                 ph[u] = make_uint4(wh[0], wh[1], wh[2], wh[3]);
                 pl[u] = make_uint4(wl[0], wl[1], wl[2], wl[3]);
@@ -298,7 +345,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
             }
 #pragma unroll
             for (int i = g * VPG; i < (g + 1) * VPG; ++i) {
-                const uint4 a = vop(x.v[i]);
+                const uint4 a = vop(xv[i]);
 #pragma unroll
                 for (int u = 0; u < QT; ++u) acc[u][i] = mfma32<kBF16>(a, ph[u], acc[u][i]);
 #pragma unroll
@@ -306,13 +353,15 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
             }
         }
         if ((++done & 7) == 0) flush();
+        }
+        load_v(next);
     }
     flush();
 
     // The waves' results: o = sum_w 2^(m_w - m) o_w, l alike, in a fixed order.
     float *part_o = reinterpret_cast<float *>(A.ws);
     float2 *part_ml = reinterpret_cast<float2 *>(part_o + (size_t)kAttnPartRows * D);
-    const size_t prow = attn_part_row(A, split, s, head, tile, R);
+    const size_t prow = attn_part_row(A, split, s, head, tile);
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         const float lw = add_swap32(add_swap16(l[u]));
@@ -355,14 +404,17 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(AttnArgs A) {
     }
 }
 
-// The splits' results of one query row per wave, in a fixed order.
+// The splits' results of one query row per workgroup, in a fixed order: D / 4 threads hold the
+// channels, the groups of them take the splits in turn.
+constexpr int kAttnMaxSplits = 1024;
 template <int DT, int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A, int R) {
-    constexpr int PL = D / kWave;
-    const int lane = lane_id();
-    const long long row = (long long)blockIdx.x * 4 + threadIdx.x / kWave;   // (sequence, new token, query head)
-    if (row >= (long long)A.s.n_seq * A.s.max_new * A.q_heads) return;
-    const int hq = (int)(row % A.q_heads), s = (int)(row / A.q_heads / A.s.max_new), i = (int)(row / A.q_heads % A.s.max_new);
+    constexpr int CT = D / 4, P = 256 / CT, PER = kAttnMaxSplits / 256;
+    __shared__ float w_sh[kAttnMaxSplits], red[8];
+    __shared__ v4f o_sh[P][CT];
+    const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
+    const int row = blockIdx.x;   // (sequence, new token, query head)
+    const int hq = row % A.q_heads, s = row / A.q_heads / A.s.max_new, i = row / A.q_heads % A.s.max_new;
     const SeqTokens sq = seq_tokens(A.s, s);
     if (i >= sq.n) return;
     const int head = hq / A.ratio, r = i * A.ratio + hq % A.ratio, tile = r / R;
@@ -370,32 +422,51 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A, int R) {
     if (sp.eff <= 1) return;
     const float *part_o = reinterpret_cast<const float *>(A.ws);
     const float2 *part_ml = reinterpret_cast<const float2 *>(part_o + (size_t)kAttnPartRows * D);
-    const size_t stride = attn_part_row(A, 1, 0, 0, 0, R), at = attn_part_row(A, 0, s, head, tile, R) + r % R;
-    float mm = kAttnNone;
-    for (int k = lane; k < sp.eff; k += kWave) mm = fmaxf(mm, part_ml[at + k * stride].x);
-    for (int x = 1; x < kWave; x <<= 1) mm = fmaxf(mm, __shfl_xor(mm, x));
-    float ll = 0.0f, o[PL] = {};
-    for (int k0 = 0; k0 < sp.eff; k0 += kWave) {
-        float f = 0.0f;
-        if (k0 + lane < sp.eff) {
-            const float2 ml = part_ml[at + (k0 + lane) * stride];
-            f = __builtin_amdgcn_exp2f(ml.x - mm);
-            ll = fmaf(ml.y, f, ll);
-        }
-        const int n = min(sp.eff - k0, kWave);
-#pragma unroll 4
-        for (int k = 0; k < n; ++k) {
-            const float w = __shfl(f, k);
-            const float *src = part_o + (at + (size_t)(k0 + k) * stride) * D + lane * PL;
+    const size_t stride = attn_part_row(A, 1, 0, 0, 0), at = attn_part_row(A, 0, s, head, tile) + r % R;
+    const int p = tid / CT, c = tid % CT;
+    const float *src = part_o + at * D + 4 * c;
+    constexpr int U = 4;
+    v4f first[U];   // asked for together with the maxima
 #pragma unroll
-            for (int e = 0; e < PL; ++e) o[e] = fmaf(w, src[e], o[e]);
-        }
+    for (int j = 0; j < U; ++j) first[j] = *reinterpret_cast<const v4f *>(src + (size_t)min(p + P * j, sp.eff - 1) * stride * D);
+    float2 ml[PER];
+    float mm = kAttnNone;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int k = tid + 256 * j;
+        ml[j] = k < sp.eff ? part_ml[at + k * stride] : make_float2(kAttnNone, 0.0f);
+        mm = fmaxf(mm, ml[j].x);
+    }
+    for (int x = 1; x < kWave; x <<= 1) mm = fmaxf(mm, __shfl_xor(mm, x));
+    if (lane == 0) red[wave] = mm;
+    __syncthreads();
+    mm = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    float ll = 0.0f;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const float f = __builtin_amdgcn_exp2f(ml[j].x - mm);
+        if (tid + 256 * j < sp.eff) w_sh[tid + 256 * j] = f;
+        ll = fmaf(ml[j].y, f, ll);
     }
     ll = wave_sum(ll);
-    const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
-    uint16_t *dst = A.out + (size_t)(sq.t0 + i) * A.ldo + (size_t)hq * D + lane * PL;
+    if (lane == 0) red[4 + wave] = ll;
+    __syncthreads();
+    ll = (red[4] + red[5]) + (red[6] + red[7]);
+    v4f o{0, 0, 0, 0};
 #pragma unroll
-    for (int e = 0; e < PL; ++e) dst[e] = float_to_half<DT>(o[e] * inv);
+    for (int j = 0; j < U; ++j)
+        if (p + P * j < sp.eff) o += w_sh[p + P * j] * first[j];
+#pragma unroll 4
+    for (int k = p + P * U; k < sp.eff; k += P) o += w_sh[k] * *reinterpret_cast<const v4f *>(src + k * stride * D);
+    o_sh[p][c] = o;
+    __syncthreads();
+    if (p > 0) return;
+#pragma unroll
+    for (int j = 1; j < P; ++j) o += o_sh[j][c];
+    const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+    const uint32_t w0 = float_to_half<DT>(o[0] * inv) | (uint32_t)float_to_half<DT>(o[1] * inv) << 16;
+    const uint32_t w1 = float_to_half<DT>(o[2] * inv) | (uint32_t)float_to_half<DT>(o[3] * inv) << 16;
+    *reinterpret_cast<uint2 *>(A.out + (size_t)(sq.t0 + i) * A.ldo + (size_t)hq * D + 4 * c) = make_uint2(w0, w1);
 }
 
 template <int DT, int D, int NG, int QT>
@@ -406,15 +477,19 @@ hipError_t run_attn(AttnArgs &a, hipStream_t s) {
     // partial results fit their area.
     const long long base = (long long)a.s.n_seq * a.c.heads * a.tiles;
     const int blocks = (a.s.max_kv + kKvBlock - 1) / kKvBlock;
-    long long n = base >= 1024 ? 1 : 1024 / base;
-    if (n > kAttnPartRows / R / base) n = kAttnPartRows / R / base;
+    static const int tv = getenv("TV") ? atoi(getenv("TV")) : 1;
+    const long long target = 256 * attn_waves(D, NG, QT) * tv;
+    long long n = target / base;
+    if (n > kAttnMaxSplits) n = kAttnMaxSplits;
+    a.part_rows = (int)((long long)a.s.max_new * a.ratio < R ? a.s.max_new * a.ratio : R);
+    if (n > kAttnPartRows / a.part_rows / base) n = kAttnPartRows / a.part_rows / base;
     if (n > (blocks + kAttnMinBlocks - 1) / kAttnMinBlocks) n = (blocks + kAttnMinBlocks - 1) / kAttnMinBlocks;
     a.splits = n < 1 ? 1 : (int)n;
     attn_kernel<DT, D, NG, QT><<<(unsigned)(base * a.splits), 64 * kAttnWaves, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     const long long rows = (long long)a.s.n_seq * a.s.max_new * a.q_heads;
-    attn_join_kernel<DT, D><<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(a, R);
+    attn_join_kernel<DT, D><<<(unsigned)rows, 256, 0, s>>>(a, R);
     return hipGetLastError();
 }
 
@@ -422,8 +497,9 @@ template <int DT, int D, int NG>
 hipError_t launch_attn_rows(AttnArgs &a, hipStream_t s) {
     const long long rows = (long long)a.s.max_new * a.ratio;
     if (rows <= 16) return run_attn<DT, D, NG, 1>(a, s);
-    if (rows <= 32 || D == 256) return run_attn<DT, D, NG, 2>(a, s);
-    return run_attn<DT, D, NG, D == 256 ? 2 : 4>(a, s);
+    static const int qv = getenv("QV") ? atoi(getenv("QV")) : 0;
+    if (qv == 1) return run_attn<DT, D, NG, 1>(a, s);
+    return run_attn<DT, D, NG, 2>(a, s);
 }
 
 template <int DT>

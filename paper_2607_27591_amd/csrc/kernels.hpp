@@ -160,10 +160,11 @@ struct AttnArgs {
     uint16_t *out;
     int64_t ldq, ldo;
     int q_heads, ratio, window;   // ratio: query heads per kv head
-    float scale;                  // times log2 e
+    float scale;                  // magnitude, times log2 e
+    uint32_t q_sign;              // 0x80008000 where the scale is negative: turns the queries round
     int page_shift;               // log2 of the blocks of a page, or -1
     void *ws;
-    int tiles, splits;            // set by the launch
+    int tiles, splits, part_rows;   // set by the launch
 };
 hipError_t launch_attn_bf16(AttnArgs &a, hipStream_t stream);
 hipError_t launch_attn_f16(AttnArgs &a, hipStream_t stream);
