@@ -32,19 +32,23 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs &A, const SeqTokens
     return s;
 }
 
-// Waves per SIMD that the registers are to allow.
-constexpr int attn_waves(int D, int NG, int QT) { return QT == 1 ? (D == 256 ? 2 : D == 128 ? 3 : 4) : QT == 2 && D <= 128 ? 2 : 1; }
+// Waves per SIMD that the registers of a variant allow without spilling.
+constexpr int attn_waves(int D, int NG, int QT) {
+    if (QT == 1) return D == 64 ? 5 : D == 128 ? (NG == 4 ? 3 : 4) : (NG == 2 ? 3 : 2);
+    return D == 64 ? (NG == 1 ? 4 : 3) : D == 128 ? (NG == 1 ? 3 : 2) : 1;
+}
 
+// A lane's W words of a half block of keys or a block of values (kv_k_word, kv_v_word).
 template <int W>
-__device__ __forceinline__ void load_words(uint32_t (&out)[W], const uint8_t *p) {
+__device__ __forceinline__ void load_words(uint32_t (&out)[W], const uint8_t *p, int lane) {
     if constexpr (W == 2) {
-        const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p));
+        const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p) + lane);
         out[0] = v[0];
         out[1] = v[1];
     } else {
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
-            const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p) + i);
+            const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p) + 64 * i + lane);
 #pragma unroll
             for (int e = 0; e < 4; ++e) out[4 * i + e] = v[e];
         }
@@ -111,7 +115,11 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
     constexpr int R = 16 * QT, KW = D / 32, VT = D / 16, SPG = KW / NG, VPG = VT / NG;
     constexpr int TC = VT < 8 ? VT : 8;   // channel tiles joined at a time
     constexpr KvLayout L(D, D / NG);
-    __shared__ v4f o_sh[kAttnWaves][TC][kWave];
+    // Queries and base as operands during the pass (read again for each block, which leaves
+    // their registers to more waves), the waves' results afterwards.
+    constexpr int QB = QT * (KW + NG), OB = kAttnWaves * TC;
+    __shared__ v4f smem[QB > OB ? QB : OB][kWave];
+    v4f (&o_sh)[QB > OB ? QB : OB][kWave] = smem;
     __shared__ float m_sh[kAttnWaves][16], l_sh[kAttnWaves][16];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int lane = lane_id(), h = lane / 16, col = lane % 16;
@@ -143,13 +151,13 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
         return A.c.blob + (ok ? at : 0);
     };
     auto load_k = [&](const uint8_t *rec) {
-        load_words(xk[0], rec + lane * (KW * 4));
-        load_words(xk[1], rec + (64 + lane) * (KW * 4));
+        load_words(xk[0], rec, lane);
+        load_words(xk[1], rec + 64 * KW * 4, lane);
 #pragma unroll
         for (int g = 0; g < NG; ++g) xks[g] = *reinterpret_cast<const u32x4 *>(rec + L.k_scales + g * 64 + h * 16);
     };
     auto load_v = [&](const uint8_t *rec) {
-        load_words(xv, rec + L.v_codes + lane * (VT * 4));
+        load_words(xv, rec + L.v_codes, lane);
 #pragma unroll
         for (int g = 0; g < NG; ++g) xvs[g] = *reinterpret_cast<const u32x4 *>(rec + L.v_scales + g * 64 + h * 16);
     };
@@ -166,24 +174,37 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
         load_v(next);
     }
     // Queries as operands, and what each lane's row may see.
-    uint4 q[QT][KW];
     int lo[QT], hi[QT];
     int lo_max = 0, hi_min = 0x7FFFFFFF;
+    const Int4Oct<DT> kop;
+    const Int4Oct<kBF16> vop;
+    const Bf16Left left;
+    const uint4 kminus = Int4Oct<DT>::minus(), vminus = Int4Oct<kBF16>::minus();
+    const v4f zero{0, 0, 0, 0};
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         const int r = min(r0 + 16 * u + col, rows - 1), i = r / A.ratio;   // past the last row: it again
         const uint16_t *p = A.q + (size_t)(sq.t0 + i) * A.ldq + (size_t)(head * A.ratio + r - i * A.ratio) * D + 8 * h;
-#pragma unroll
-        for (int w = 0; w < KW; ++w) {
-            q[u][w] = *reinterpret_cast<const uint4 *>(p + 32 * w);
-            q[u][w].x ^= A.q_sign;
-            q[u][w].y ^= A.q_sign;
-            q[u][w].z ^= A.q_sign;
-            q[u][w].w ^= A.q_sign;
+        for (int w = wave; w < KW; w += kAttnWaves) {
+            uint4 v = *reinterpret_cast<const uint4 *>(p + 32 * w);
+            v.x ^= A.q_sign;
+            v.y ^= A.q_sign;
+            v.z ^= A.q_sign;
+            v.w ^= A.q_sign;
+            smem[u * KW + w][lane] = __builtin_bit_cast(v4f, v);
         }
         hi[u] = sq.pos0 + i;
         lo[u] = A.window > 0 ? hi[u] - A.window + 1 : 0;
     }
+    __syncthreads();
+    for (int ug = wave; ug < QT * NG; ug += kAttnWaves) {
+        v4f d = zero;
+#pragma unroll
+        for (int w = 0; w < SPG; ++w)
+            d = mfma32<DT>(kminus, __builtin_bit_cast(uint4, smem[ug / NG * KW + ug % NG * SPG + w][lane]), d);
+        smem[QT * KW + ug][lane] = d;
+    }
+    __syncthreads();
     {   // over the tile's rows, from its first and last
         const int i0 = r0 / A.ratio, i1 = (min(r0 + R, rows) - 1) / A.ratio;
         hi_min = sq.pos0 + i0;
@@ -192,20 +213,6 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
     const int hi_max = sq.pos0 + (min(r0 + R, rows) - 1) / A.ratio;
     const int lo_min = A.window > 0 ? hi_min - A.window + 1 : 0;
 
-    const Int4Oct<DT> kop;
-    const Int4Oct<kBF16> vop;
-    const Bf16Left left;
-    const uint4 kminus = Int4Oct<DT>::minus(), vminus = Int4Oct<kBF16>::minus();
-    const v4f zero{0, 0, 0, 0};
-    v4f base[QT][NG];
-#pragma unroll
-    for (int u = 0; u < QT; ++u)
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            base[u][g] = zero;
-#pragma unroll
-            for (int w = g * SPG; w < (g + 1) * SPG; ++w) base[u][g] = mfma32<DT>(kminus, q[u][w], base[u][g]);
-        }
     v4f acc[QT][VT], acc_off[QT][NG];
     // Running maximum m of scale times the score; a score above top raises it.
     float m[QT], l[QT], top[QT];
@@ -237,26 +244,34 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
         next_id = page_id(b + 2 * kAttnWaves);
         float sc[QT][2][4];
         if (ok) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
+            asm volatile("" ::: "memory");   // the queries stay in LDS
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                v4f d[QT];
+                v4f d[QT][2];
+#pragma unroll
+                for (int u = 0; u < QT; ++u) d[u][0] = d[u][1] = smem[QT * KW + u * NG + g][lane];
 #pragma unroll
                 for (int w = g * SPG; w < (g + 1) * SPG; ++w) {
-                    const uint4 a = kop(xk[j][w]);
+                    uint4 q[QT];
 #pragma unroll
-                    for (int u = 0; u < QT; ++u) d[u] = mfma32<DT>(a, q[u][w], w == g * SPG ? base[u][g] : d[u]);
+                    for (int u = 0; u < QT; ++u) q[u] = __builtin_bit_cast(uint4, smem[u * KW + w][lane]);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint4 a = kop(xk[j][w]);
+#pragma unroll
+                        for (int u = 0; u < QT; ++u) d[u][j] = mfma32<DT>(a, q[u], d[u][j]);
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < QT; ++u)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float f = slot_scale(xks[g], j, e);
-                        sc[u][j][e] = g == 0 ? times(d[u][e], f) : fmaf(d[u][e], f, sc[u][j][e]);
-                    }
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float f = slot_scale(xks[g], j, e);
+                            sc[u][j][e] = g == 0 ? times(d[u][j][e], f) : fmaf(d[u][j][e], f, sc[u][j][e]);
+                        }
             }
-        }
         }
         load_k(next);
         if (ok) {
@@ -385,12 +400,12 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
         for (int c = 0; c < VT; c += TC) {
             if (c > 0) __syncthreads();
 #pragma unroll
-            for (int i2 = 0; i2 < TC; ++i2) o_sh[wave][i2][lane] = acc[u][c + i2] * f;
+            for (int i2 = 0; i2 < TC; ++i2) o_sh[wave * TC + i2][lane] = acc[u][c + i2] * f;
             __syncthreads();
             for (int i2 = wave; i2 < TC; i2 += kAttnWaves) {
-                v4f o = o_sh[0][i2][lane];
+                v4f o = o_sh[i2][lane];
 #pragma unroll
-                for (int w = 1; w < kAttnWaves; ++w) o += o_sh[w][i2][lane];
+                for (int w = 1; w < kAttnWaves; ++w) o += o_sh[w * TC + i2][lane];
                 if (r >= rows) continue;
                 if (sp.eff > 1) {
                     *reinterpret_cast<v4f *>(part_o + (prow + 16 * u + col) * D + 16 * (c + i2) + 4 * h) = o;
@@ -496,10 +511,11 @@ hipError_t run_attn(AttnArgs &a, hipStream_t s) {
 template <int DT, int D, int NG>
 hipError_t launch_attn_rows(AttnArgs &a, hipStream_t s) {
     const long long rows = (long long)a.s.max_new * a.ratio;
-    if (rows <= 16) return run_attn<DT, D, NG, 1>(a, s);
-    static const int qv = getenv("QV") ? atoi(getenv("QV")) : 0;
-    if (qv == 1) return run_attn<DT, D, NG, 1>(a, s);
-    return run_attn<DT, D, NG, 2>(a, s);
+    if constexpr (D < 256) {
+        static const int qv = getenv("QV") ? atoi(getenv("QV")) : 16;
+        if (rows > qv) return run_attn<DT, D, NG, 2>(a, s);
+    }
+    return run_attn<DT, D, NG, 1>(a, s);
 }
 
 template <int DT>

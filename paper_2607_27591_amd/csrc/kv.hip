@@ -159,16 +159,15 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs A) {
         if (ch % span == 0)
             *reinterpret_cast<uint16_t *>(rec + (keys ? L.k_scales : L.v_scales) + (ch / span) * 64 + kv_slot(t) * 2) = sc.bits;
         if (keys)
-            *reinterpret_cast<uint32_t *>(rec + (size_t)(((t / 16) * 64 + (ch % 4) * 16 + t % 16) * (D / 32) + ch / 4) * 4) =
+            *reinterpret_cast<uint32_t *>(rec + kv_k_word(D, t, ch) * 4) =
                 code_word<DT>(v, sc, [](int e) { return nibble_of(e); });
         else
             vcodes[t][ch] = code_word<DT>(v, sc, [](int e) { return e; });
     }
     __syncthreads();
-    // Word w of the V codes: lane w / (D / 16), channel 16 (w % (D / 16)) + lane % 16.
     uint32_t *words = reinterpret_cast<uint32_t *>(rec + L.v_codes);
     for (int w = tid; w < 4 * D; w += 256) {
-        const int lane = w / (D / 16), c = (w % (D / 16)) * 16 + lane % 16, h = lane / 16;
+        const int lane = w / 4 % 64, c = (w / 256 * 4 + w % 4) * 16 + lane % 16, h = lane / 16;   // kv_v_word(lane, c / 16) == w
         uint32_t mask = 0, codes = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -201,13 +200,13 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvCache c, KvSeqs q, float
         const float ks = f16_bits_to_float(*reinterpret_cast<const uint16_t *>(rec + L.k_scales + g * 64 + kv_slot(t) * 2));
         const float vs = f16_bits_to_float(*reinterpret_cast<const uint16_t *>(rec + L.v_scales + g * 64 + kv_slot(t) * 2));
         const uint32_t kw = *reinterpret_cast<const uint32_t *>(
-            rec + (size_t)(((t / 16) * 64 + (ch % 4) * 16 + t % 16) * (c.dim / 32) + ch / 4) * 4);
+            rec + kv_k_word(c.dim, t, ch) * 4);
         const int lane0 = ((t % 16) / 4) * 16, nib = t % 4 + 4 * (t / 16);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int cc = 8 * ch + e;
             const uint32_t vw = *reinterpret_cast<const uint32_t *>(
-                rec + L.v_codes + (size_t)((lane0 + cc % 16) * (c.dim / 16) + cc / 16) * 4);
+                rec + L.v_codes + kv_v_word(lane0 + cc % 16, cc / 16) * 4);
             kv[e] = ks * (float)((int)((kw >> (4 * nibble_of(e))) & 15) - 8);
             vv[e] = vs * (float)((int)((vw >> (4 * nib)) & 15) - 8);
         }

@@ -252,15 +252,24 @@ struct LinearLayout {
 // 4-bit paged key/value cache
 // ---------------------------------------------------------------------------
 // [page][kv head][block of 32 tokens of the page] records, each of
-//   K codes   [token / 16][lane 0..63][D / 32 words]: lane l holds token l % 16 of the
-//             half block, word i channels 32 i + 8 (l / 16) .. + 7 (nibble_of)
-//   V codes   [lane 0..63][D / 16 words]: lane l, word i holds channel 16 i + l % 16, at
+//   K codes   [token / 16][word / 4][lane 0..63][4 words] (head_dim 64: 2 words): lane l holds
+//             token l % 16 of the half block, word i channels 32 i + 8 (l / 16) .. + 7 (nibble_of)
+//   V codes   [word / 4][lane 0..63][4 words]: lane l, word i holds channel 16 i + l % 16, at
 //             nibble j token 4 (l / 16) + j (j < 4), 16 + 4 (l / 16) + j - 4 (j >= 4)
 //   K scales  [group][kv_slot(token)] fp16 bits;   V scales alike
 // so that a lane's words are its MFMA operands of both products (queries times keys, and
-// values times probabilities as the first product leaves them), its four runs of scales
-// those of the tokens whose scores it gets, and a record one contiguous run.
+// values times probabilities as the first product leaves them), a load of 16 bytes a lane is
+// one run of 1024 bytes, a run of scales is that of the 8 tokens whose scores a lane gets, and
+// a record is one contiguous run.
 constexpr int kKvBlock = 32;
+
+// Word of the K codes that holds channels 8 ch .. 8 ch + 7 of token t, and of the V codes that
+// is word i of a lane.
+__host__ __device__ constexpr int kv_k_word(int head_dim, int t, int ch) {
+    const int kw = head_dim / 32, g = kw < 4 ? kw : 4, w = ch / 4;
+    return (((t / 16) * (kw / g) + w / g) * 64 + (ch % 4) * 16 + t % 16) * g + w % g;
+}
+__host__ __device__ constexpr int kv_v_word(int lane, int i) { return ((i / 4) * 64 + lane) * 4 + i % 4; }
 
 // Place of token t of a block in a row of scales: the 8 tokens of lanes 16 h .. 16 h + 15 together.
 __host__ __device__ constexpr int kv_slot(int t) { return ((t >> 2) & 3) * 8 + (t >> 4) * 4 + (t & 3); }

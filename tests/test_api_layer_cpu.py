@@ -161,10 +161,9 @@ int main() {
         for (int t = 0; t < 32; ++t)
             for (int c = 0; c < D; ++c) {
                 const int ch = c / 8, e = c % 8;
-                const int word = ((t / 16) * 64 + (ch % 4) * 16 + t % 16) * (D / 32) + ch / 4;
-                ++k.at(word * 8 + nibble_of(e));
+                ++k.at(kv_k_word(D, t, ch) * 8 + nibble_of(e));
                 const int lane = ((t % 16) / 4) * 16 + c % 16;
-                ++v.at((lane * (D / 16) + c / 16) * 8 + t % 4 + 4 * (t / 16));
+                ++v.at(kv_v_word(lane, c / 16) * 8 + t % 4 + 4 * (t / 16));
             }
         for (int i = 0; i < 32 * D; ++i) need(k[i] == 1 && v[i] == 1, "codes");
     }
