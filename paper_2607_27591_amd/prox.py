@@ -554,23 +554,45 @@ def add_rmsnorm(x: torch.Tensor, y: torch.Tensor, eps: float = 1e-6,
 # The attention half of a decoder layer
 # ---------------------------------------------------------------------------
 
+# These calls sit between small kernels of a decode step, so they keep their own cost low:
+# a handle's C struct is built once (and again if its tensor's memory has moved), pointers go
+# as integers.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _on(device: torch.device, f, *args) -> int:
     """f(*args, stream) on the current stream of `device`, which may not be the
     current device."""
-    if device.index is None or device.index == torch.cuda.current_device():
-        return f(*args, _stream(device))
-    with torch.cuda.device(device):
-        return f(*args, _stream(device))
+    index = device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return f(*args, torch.cuda.current_stream(device).cuda_stream)
+    return f(*args, torch.cuda.current_stream(device).cuda_stream if _raw_stream is None else _raw_stream(index))
 
 
-def _same_device(device: torch.device, **tensors) -> None:
-    for what, t in tensors.items():
+def _at(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _same_device(device: torch.device, *tensors) -> None:
+    for t in tensors:
         if t is not None and t.device != device:
-            raise ValueError(f"{what} is on {t.device}, not on {device}")
+            raise ValueError(f"every tensor of a call must be on one device: {t.device} and {device}")
 
 
-@dataclasses.dataclass
-class LinearW4:
+class _Handle:
+    """Keeps the C struct of an immutable dataclass, as a pointer to pass."""
+
+    def _pointer(self, *key):
+        kept = self.__dict__.get("_kept")
+        if kept is None or kept[0] != key:
+            kept = (key, ctypes.byref(self.struct()))
+            object.__setattr__(self, "_kept", kept)
+        return kept[1]
+
+
+@dataclasses.dataclass(frozen=True)
+class LinearW4(_Handle):
     """A projection's weights in INT4 (W4A16): an opaque device blob."""
     blob: torch.Tensor
     dtype: torch.dtype
@@ -582,6 +604,9 @@ class LinearW4:
         _dev_tensor(self.blob, "linear blob", torch.uint8)
         return _W4Linear(_TORCH_DT[self.dtype], self.n, self.k, self.group, self.blob.data_ptr(),
                          self.blob.numel())
+
+    def pointer(self):
+        return self._pointer(self.blob.data_ptr(), self.blob.numel())
 
 
 def linear_w4_bytes(n: int, k: int, group: int = 128) -> int:
@@ -600,8 +625,7 @@ def pack_linear_w4(w: torch.Tensor, group: int = 128) -> LinearW4:
     if size == 0:
         raise ProxError(2, "prox_linear_w4_bytes")
     q = LinearW4(torch.empty(size, dtype=torch.uint8, device=w.device), w.dtype, n, k, group)
-    qs = q.struct()
-    _check(_on(w.device, lib().prox_pack_linear_w4, _ptr(w), ctypes.byref(qs)), "prox_pack_linear_w4")
+    _check(_on(w.device, lib().prox_pack_linear_w4, _at(w), q.pointer()), "prox_pack_linear_w4")
     return q
 
 
@@ -610,48 +634,46 @@ def unpack_linear_w4(q: LinearW4):
     dev = q.blob.device
     codes = torch.empty((q.n, q.k), dtype=torch.int8, device=dev)
     scales = torch.empty((q.n, q.k // q.group), dtype=torch.int16, device=dev)
-    qs = q.struct()
-    _check(_on(dev, lib().prox_unpack_linear_w4, ctypes.byref(qs), _ptr(codes), _ptr(scales)),
+    _check(_on(dev, lib().prox_unpack_linear_w4, q.pointer(), _at(codes), _at(scales)),
            "prox_unpack_linear_w4")
     return codes, scales
 
 
-def _rows2(t: torch.Tensor, what: str, dtype: torch.dtype, cols: int) -> int:
-    """Row stride of a [rows][cols] device tensor whose rows may stand apart."""
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+def _rows2(t: torch.Tensor, what: str, dtype: torch.dtype, cols: int):
+    """(rows, row stride) of a device tensor [rows][cols], or [cols], whose rows may stand apart."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{what} must be a CUDA (HIP) tensor")
     if t.dtype != dtype:
         raise ValueError(f"{what} must have dtype {dtype}, got {t.dtype}")
-    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+    shape, stride = t.shape, t.stride()
+    if not 1 <= len(shape) <= 2 or shape[-1] != cols or (cols > 1 and stride[-1] != 1):
         raise ValueError(f"{what} must be [rows][{cols}] with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else cols
+    return (shape[0], stride[0]) if len(shape) == 2 and shape[0] != 1 else (1, cols)
 
 
 def linear_w4(q: LinearW4, x: torch.Tensor, bias: Optional[torch.Tensor] = None,
               y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [batch][k] (or [k]) times the INT4 weights, plus bias [n]; rows of x and y may
     stand apart (parts of wider tensors)."""
-    x2 = x.unsqueeze(0) if x.dim() == 1 else x
-    ldx = _rows2(x2, "x", q.dtype, q.k)
+    batch, ldx = _rows2(x, "x", q.dtype, q.k)
+    dev = x.device
     if y is None:
-        y = torch.empty(x.shape[:-1] + (q.n,), dtype=q.dtype, device=x.device)
-    y2 = y.unsqueeze(0) if y.dim() == 1 else y
-    ldy = _rows2(y2, "y", q.dtype, q.n)
-    if y2.shape[0] != x2.shape[0]:
+        y = torch.empty(x.shape[:-1] + (q.n,), dtype=q.dtype, device=dev)
+    rows, ldy = _rows2(y, "y", q.dtype, q.n)
+    if rows != batch:
         raise ValueError("y must have the rows of x")
     if bias is not None:
         _dev_tensor(bias, "bias", q.dtype)
         if bias.numel() != q.n:
             raise ValueError("bias must be [n]")
-    _same_device(x.device, blob=q.blob, y=y, bias=bias)
-    qs = q.struct()
-    _check(_on(x.device, lib().prox_linear_w4, ctypes.byref(qs), _ptr(x), ldx, x2.shape[0], _ptr(bias),
-               _ptr(y), ldy), "prox_linear_w4")
+    _same_device(dev, q.blob, y, bias)
+    _check(_on(dev, lib().prox_linear_w4, q.pointer(), x.data_ptr(), ldx, batch, _at(bias), y.data_ptr(), ldy),
+           "prox_linear_w4")
     return y
 
 
-@dataclasses.dataclass
-class KVCache:
+@dataclasses.dataclass(frozen=True)
+class KVCache(_Handle):
     """Paged key/value cache in 4 bits: an opaque device blob."""
     blob: torch.Tensor
     dtype: torch.dtype
@@ -665,6 +687,9 @@ class KVCache:
         _dev_tensor(self.blob, "cache blob", torch.uint8)
         return _KVCache(_TORCH_DT[self.dtype], self.kv_heads, self.head_dim, self.group, self.page_size,
                         self.n_pages, self.blob.data_ptr(), self.blob.numel())
+
+    def pointer(self):
+        return self._pointer(self.blob.data_ptr(), self.blob.numel())
 
 
 def kv_bytes(kv_heads: int, head_dim: int, group: int, page_size: int, n_pages: int) -> int:
@@ -682,7 +707,7 @@ def new_kv_cache(n_pages: int, page_size: int, kv_heads: int, head_dim: int, dty
                    page_size, n_pages)
 
 
-@dataclasses.dataclass
+@dataclasses.dataclass(frozen=True)
 class KVSeqs:
     """The sequences of a call (prox_kv_seqs): device int32 kv_len [n_seq] (the new
     tokens included), page_table [n_seq][max_pages] and, where sequences have unequal
@@ -694,7 +719,7 @@ class KVSeqs:
     cu_new: Optional[torch.Tensor] = None
     max_kv: int = 0
 
-    def struct(self, n_tokens: int) -> _KVSeqs:
+    def struct(self, n_tokens: int = 0) -> _KVSeqs:
         _dev_tensor(self.kv_len, "kv_len", torch.int32)
         _dev_tensor(self.page_table, "page_table", torch.int32)
         n = self.kv_len.numel()
@@ -704,13 +729,23 @@ class KVSeqs:
             _dev_tensor(self.cu_new, "cu_new", torch.int32)
             if self.cu_new.numel() != n + 1:
                 raise ValueError("cu_new must be [n_seq + 1]")
-        return _KVSeqs(n, self.max_new, n_tokens, self.max_kv, self.page_table.shape[1],
-                       None if self.cu_new is None else self.cu_new.data_ptr(), self.kv_len.data_ptr(),
-                       self.page_table.data_ptr())
+        return _KVSeqs(n, self.max_new, n_tokens, self.max_kv, self.page_table.shape[1], _at(self.cu_new),
+                       self.kv_len.data_ptr(), self.page_table.data_ptr())
+
+    def pointer(self, device: torch.device, n_tokens: int):
+        """For a call of n_tokens rows on `device`."""
+        key = (device, n_tokens, self.kv_len.data_ptr(), self.page_table.data_ptr(), _at(self.cu_new),
+               self.kv_len.shape, self.page_table.shape)
+        kept = self.__dict__.get("_kept")
+        if kept is None or kept[0] != key:
+            _same_device(device, self.kv_len, self.page_table, self.cu_new)
+            kept = (key, ctypes.byref(self.struct(n_tokens)))
+            object.__setattr__(self, "_kept", kept)
+        return kept[1]
 
 
-@dataclasses.dataclass
-class Rope:
+@dataclasses.dataclass(frozen=True)
+class Rope(_Handle):
     """Rotation table, device float32 [n_pos][dim]: dim / 2 cosines, then the sines, of
     every position; pairs (i, i + dim / 2), or (2 i, 2 i + 1) if interleaved."""
     table: torch.Tensor
@@ -722,18 +757,21 @@ class Rope:
             raise ValueError("rope table must be [n_pos][dim]")
         return _Rope(self.table.data_ptr(), self.table.shape[0], self.table.shape[1], int(self.interleaved))
 
+    def pointer(self):
+        return self._pointer(self.table.data_ptr(), self.table.shape)
 
-def _heads(t: torch.Tensor, what: str, c: KVCache, heads: Optional[int] = None) -> int:
-    """Token stride of a [tokens][heads][head_dim] device tensor."""
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+
+def _heads(t: torch.Tensor, what: str, c: KVCache, heads: int = 0):
+    """(tokens, heads, token stride) of a device tensor [tokens][heads][head_dim]."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{what} must be a CUDA (HIP) tensor")
     if t.dtype != c.dtype:
         raise ValueError(f"{what} must have dtype {c.dtype}, got {t.dtype}")
-    if (t.dim() != 3 or t.shape[2] != c.head_dim or (heads is not None and t.shape[1] != heads) or
-            t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != c.head_dim)):
-        raise ValueError(f"{what} must be [tokens][{'heads' if heads is None else heads}][{c.head_dim}] "
-                         "with the heads of a token contiguous")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * c.head_dim
+    shape, stride, d = t.shape, t.stride(), c.head_dim
+    if (len(shape) != 3 or shape[2] != d or (heads and shape[1] != heads) or stride[2] != 1 or
+            (shape[1] > 1 and stride[1] != d)):
+        raise ValueError(f"{what} must be [tokens][{heads or 'heads'}][{d}] with the heads of a token contiguous")
+    return shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1] * d
 
 
 def kv_append(c: KVCache, s: KVSeqs, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
@@ -741,26 +779,23 @@ def kv_append(c: KVCache, s: KVSeqs, k: torch.Tensor, v: torch.Tensor, q: Option
     """Append the new tokens' k and v [tokens][kv_heads][head_dim] to the cache, rotated by
     rope if given.  Returns the rotated queries (q_out, which may be q; made here when
     not given), None without q."""
-    T = k.shape[0]
-    ldk, ldv = _heads(k, "k", c, c.kv_heads), _heads(v, "v", c, c.kv_heads)
-    if v.shape[0] != T:
-        raise ValueError("v must have the tokens of k")
+    T, _, ldk = _heads(k, "k", c, c.kv_heads)
+    tv, _, ldv = _heads(v, "v", c, c.kv_heads)
+    tq = to = T
     ldq = ldo = heads = 0
+    dev = k.device
     if q is not None:
-        ldq, heads = _heads(q, "q", c), q.shape[1]
+        tq, heads, ldq = _heads(q, "q", c)
         if q_out is None:   # rows without a place are not written
             q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-        ldo = _heads(q_out, "q_out", c, heads)
-        if q.shape[0] != T or q_out.shape[0] != T:
-            raise ValueError("q and q_out must have the tokens of k")
+        to, _, ldo = _heads(q_out, "q_out", c, heads)
     elif q_out is not None:
         raise ValueError("q_out without q")
-    _same_device(k.device, blob=c.blob, v=v, q=q, q_out=q_out, kv_len=s.kv_len, page_table=s.page_table,
-                 cu_new=s.cu_new, rope=None if rope is None else rope.table)
-    cs, ss = c.struct(), s.struct(T)
-    rs = None if rope is None else ctypes.byref(rope.struct())
-    _check(_on(k.device, lib().prox_kv_append, ctypes.byref(cs), ctypes.byref(ss), _ptr(k), ldk, _ptr(v), ldv,
-               _ptr(q), heads, ldq, _ptr(q_out), ldo, rs), "prox_kv_append")
+    if not T == tv == tq == to:
+        raise ValueError("k, v, q and q_out must have the same tokens")
+    _same_device(dev, c.blob, v, q, q_out, None if rope is None else rope.table)
+    _check(_on(dev, lib().prox_kv_append, c.pointer(), s.pointer(dev, T), k.data_ptr(), ldk, v.data_ptr(), ldv,
+               _at(q), heads, ldq, _at(q_out), ldo, None if rope is None else rope.pointer()), "prox_kv_append")
     return q_out
 
 
@@ -779,9 +814,9 @@ def kv_read(c: KVCache, s: KVSeqs, k: Optional[torch.Tensor] = None, v: Optional
     v = torch.zeros(shape, dtype=torch.float32, device=dev) if v is None else _dev_tensor(v, "v", torch.float32)
     if tuple(k.shape) != shape or tuple(v.shape) != shape:
         raise ValueError("k and v must be [n_tokens][kv_heads][head_dim]")
-    _same_device(dev, k=k, v=v, kv_len=s.kv_len, page_table=s.page_table, cu_new=s.cu_new)
-    cs, ss = c.struct(), s.struct(n_tokens)
-    _check(_on(dev, lib().prox_kv_read, ctypes.byref(cs), ctypes.byref(ss), _ptr(k), _ptr(v)), "prox_kv_read")
+    _same_device(dev, k, v)
+    _check(_on(dev, lib().prox_kv_read, c.pointer(), s.pointer(dev, n_tokens), k.data_ptr(), v.data_ptr()),
+           "prox_kv_read")
     return k, v
 
 
@@ -801,19 +836,18 @@ def kv_attn(c: KVCache, s: KVSeqs, q: torch.Tensor, scale: Optional[float] = Non
     """Attention of the new tokens' queries [tokens][q_heads][head_dim] over the cache
     (which holds the tokens' own keys and values already).  scale: head_dim ** -0.5 when
     not given; window > 0: the last `window` positions only."""
-    ldq = _heads(q, "q", c)
+    T, heads, ldq = _heads(q, "q", c)
+    dev = q.device
     if out is None:   # rows of no sequence are not written
-        out = (torch.empty if s.cu_new is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
-    ldo = _heads(out, "out", c, q.shape[1])
-    if out.shape[0] != q.shape[0]:
+        out = (torch.empty if s.cu_new is None else torch.zeros)(q.shape, dtype=q.dtype, device=dev)
+    rows, _, ldo = _heads(out, "out", c, heads)
+    if rows != T:
         raise ValueError("out must have the tokens of q")
-    ws = new_kv_attn_workspace(c.head_dim, q.device) if ws is None else _dev_tensor(ws, "ws", torch.uint8)
-    _same_device(q.device, blob=c.blob, out=out, ws=ws, kv_len=s.kv_len, page_table=s.page_table,
-                 cu_new=s.cu_new)
-    cs, ss = c.struct(), s.struct(q.shape[0])
-    _check(_on(q.device, lib().prox_kv_attn, ctypes.byref(cs), ctypes.byref(ss), _ptr(q), q.shape[1], ldq,
-               c.head_dim ** -0.5 if scale is None else float(scale), int(window), _ptr(out), ldo, _ptr(ws),
-               ws.numel()), "prox_kv_attn")
+    ws = new_kv_attn_workspace(c.head_dim, dev) if ws is None else _dev_tensor(ws, "ws", torch.uint8)
+    _same_device(dev, c.blob, out, ws)
+    _check(_on(dev, lib().prox_kv_attn, c.pointer(), s.pointer(dev, T), q.data_ptr(), heads, ldq,
+               c.head_dim ** -0.5 if scale is None else float(scale), int(window), out.data_ptr(), ldo,
+               ws.data_ptr(), ws.numel()), "prox_kv_attn")
     return out
 
 

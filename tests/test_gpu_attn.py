@@ -124,8 +124,7 @@ def test_rows_past_max_new_and_bad_pages():
     case.table[0, 4] = case.c.n_pages
     case.table[1] = 1 << 30          # all of sequence 1
     out = torch.full_like(case.q, 5.0)
-    s = case.seqs()
-    s.max_new = 3
+    s = prox.KVSeqs(case.kv_len, case.table, max_new=3, cu_new=starts(case.news))
     prox.kv_attn(case.c, s, case.q, out=out)
     hidden = np.zeros(200, bool)
     hidden[64:96] = hidden[128:160] = True
