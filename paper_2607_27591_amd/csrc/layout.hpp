@@ -229,7 +229,9 @@ __host__ __device__ inline size_t ws_bytes_up_to(int d, int f, int batch, int wq
 //         + 7 of the block, in the order of kNibble: a lane's word is its operand of
 //         one 16 x 16 x 32 MFMA, and a wave's load of a block one run of 1024 bytes.
 //         Rows past n and inputs past k hold code 0 (q + 8 = 8).
-// scales  (256-aligned) [row tile][k / group][16] fp16 bits, 0 past n.
+// scales  (256-aligned) fp16 bits, 0 past n: groups of 128 and more [row tile][k / group][16
+//         rows]; smaller ones [row tile][block][4 rows a lane gets][group of the block][4], 0 past
+//         k, so that a lane reads what it needs of a block in one run.
 constexpr int kLinearRows = 16;
 constexpr int kLinearBlock = 128;
 
@@ -238,13 +240,19 @@ constexpr int kLinearBlock = 128;
 __host__ __device__ constexpr int nibble_of(int e) { return (e >> 1) + 4 * (e & 1); }
 
 struct LinearLayout {
-    int tiles, blocks, groups;
+    int tiles, blocks, groups, gpb;   // groups of a row; of a block, at least 1
     size_t scales, total;
     __host__ __device__ LinearLayout(int n, int k, int group)
         : tiles((n + kLinearRows - 1) / kLinearRows), blocks((k + kLinearBlock - 1) / kLinearBlock),
-          groups(k / group) {
+          groups(k / group), gpb(group < kLinearBlock ? kLinearBlock / group : 1) {
         scales = (size_t)tiles * blocks * 1024;
-        total = align_up(scales + (size_t)tiles * groups * kLinearRows * 2, 256);
+        total = align_up(scales + (size_t)tiles * tile_scales() * 2, 256);
+    }
+    __host__ __device__ size_t tile_scales() const {   // values of a row tile
+        return (size_t)(gpb > 1 ? blocks * gpb : groups) * kLinearRows;
+    }
+    __host__ __device__ size_t scale_at(int tile, int g, int row) const {
+        return tile * tile_scales() + ((size_t)(g / gpb * 4 + row / 4) * gpb + g % gpb) * 4 + row % 4;
     }
 };
 

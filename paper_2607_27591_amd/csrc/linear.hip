@@ -17,7 +17,7 @@ __global__ __launch_bounds__(256) void pack_linear_kernel(const uint16_t *__rest
     const int first = (int)blockIdx.y * unit;
     const int j = tile * kLinearRows + r;
     const uint16_t *src = w + (size_t)j * k;
-    uint16_t *scales = reinterpret_cast<uint16_t *>(blob + L.scales) + (size_t)tile * L.groups * kLinearRows + r;
+    uint16_t *scales = reinterpret_cast<uint16_t *>(blob + L.scales);
     auto load = [&](int i) {   // past the matrix: zeros
         return j < n && i < k ? *reinterpret_cast<const uint4 *>(src + i) : make_uint4(0, 0, 0, 0);
     };
@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256) void pack_linear_kernel(const uint16_t *__rest
     for (int m = 1; m < span; m <<= 1) a = max(a, (uint32_t)__shfl_xor((int)a, m));
     const GroupScale s = group_scale<DT>(a, 7);
     const int g = (first + 8 * l) / group;
-    if (l % span == 0 && g < L.groups) scales[(size_t)g * kLinearRows] = s.bits;
+    if (l % span == 0) scales[L.scale_at(tile, g, r)] = s.bits;   // of zeros past n and k: 0
     for (int i = 0; i < unit; i += kLinearBlock) {
         if (i > 0) v = load(first + i + 8 * l);
         uint32_t word = 0;
@@ -60,8 +60,8 @@ __global__ __launch_bounds__(256) void unpack_linear_kernel(const uint8_t *__res
     for (int e = 0; e < 8; ++e) codes[id * 8 + e] = (int8_t)((int)((word >> (4 * nibble_of(e))) & 15) - 8);
     const int g = ch * 8 / group;
     if (ch * 8 % group == 0)
-        scales[(size_t)j * L.groups + g] = reinterpret_cast<const uint16_t *>(
-            blob + L.scales)[((size_t)(j / kLinearRows) * L.groups + g) * kLinearRows + j % kLinearRows];
+        scales[(size_t)j * L.groups + g] =
+            reinterpret_cast<const uint16_t *>(blob + L.scales)[L.scale_at(j / kLinearRows, g, j % kLinearRows)];
 }
 
 hipError_t launch_pack_linear(int dtype, const void *w, int n, int k, int group, void *blob, hipStream_t s) {

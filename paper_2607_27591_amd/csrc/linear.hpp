@@ -34,6 +34,8 @@ template <int DT, int NT, int RG, int WN, int GPB, bool TAIL>
 __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A) {
     constexpr int MT = (RG + 3) / 4, WK = kLinearWaves / WN, TILES = NT * MT, RT = TILES < 8 ? TILES : 8;
     static_assert(RG % WN == 0, "the waves of a block load the same number of rows");
+    // Steps that loads run ahead: a short k is asked for at once, many rows of x take the registers.
+    constexpr int DEPTH = 2;
     constexpr int XL = RG / WN;                     // loads of 4 rows of a block by each of its waves
     constexpr int STAGE = WK * MT * 256;            // 16-byte chunks of x: [slot][row tile][chunk of the row][row ^ chunk]
     extern __shared__ __align__(16) unsigned char smem[];
@@ -57,29 +59,38 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
     for (int t = 0; t < NT; ++t) {   // past the last tile: the last again, not stored
         const int tile = min(tile0 + t, L.tiles - 1);
         codes[t] = A.blob + (size_t)tile * L.blocks * 1024 + lane * 16;
-        scales[t] = reinterpret_cast<const uint16_t *>(A.blob + L.scales) + (size_t)tile * L.groups * kLinearRows + 4 * h;
+        scales[t] = reinterpret_cast<const uint16_t *>(A.blob + L.scales) + tile * L.tile_scales() + 4 * GPB * h;
     }
     v4f acc[NT][MT];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[t][m] = v4f{0, 0, 0, 0};
-    u32x4 c[2][NT], xv[2][XL];   // of even and odd steps, two steps ahead
-    u32x2 sc[2][NT][GPB];
-    const int last = L.blocks - 1;
-    auto load_codes = [&](int b, u32x4 (&cv)[NT], u32x2 (&sv)[NT][GPB]) {   // past the end: the last block again
-        b = min(b, last);
+    u32x4 c[DEPTH][NT], xv[DEPTH][XL];   // of step j in set j % DEPTH, DEPTH steps ahead
+    u32x2 sc[DEPTH][NT][GPB];
+    auto load_codes = [&](int b, u32x4 (&cv)[NT], u32x2 (&sv)[NT][GPB]) {
+        if (b >= L.blocks) return;
 #pragma unroll
         for (int t = 0; t < NT; ++t) cv[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(codes[t] + (size_t)b * 1024));
-        const int g0 = GPB == 1 ? (int)((uint32_t)b * A.per_group >> 20) : b * GPB;
+        const uint32_t unit = GPB == 1 ? (uint32_t)b * A.per_group >> 20 : (uint32_t)b;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t) {
+            const uint16_t *p = scales[t] + (size_t)unit * GPB * kLinearRows;
+            if constexpr (GPB == 1) {
+                sv[t][0] = *reinterpret_cast<const u32x2 *>(p);
+            } else {
 #pragma unroll
-            for (int g = 0; g < GPB; ++g)
-                sv[t][g] = *reinterpret_cast<const u32x2 *>(scales[t] + (size_t)(TAIL ? min(g0 + g, L.groups - 1) : g0 + g) * kLinearRows);
+                for (int g = 0; g < GPB; g += 2) {
+                    const u32x4 v = *reinterpret_cast<const u32x4 *>(p + 4 * g);
+                    sv[t][g] = u32x2{v[0], v[1]};
+                    sv[t][g + 1] = u32x2{v[2], v[3]};
+                }
+            }
+        }
     };
     auto load_x = [&](int b, u32x4 (&v)[XL]) {
-        const int k0 = min(b, last) * kLinearBlock;
+        if (b >= L.blocks) return;
+        const int k0 = b * kLinearBlock;
         const bool in = !TAIL || k0 + 8 * col < k;
 #pragma unroll
         for (int l = 0; l < XL; ++l) {
@@ -95,9 +106,9 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
         }
     };
     // Step j (blocks j WK + slot) computes from its LDS buffer, asks for the codes of step
-    // j + 2, stages the x of step j + 1 and asks for that of step j + 3.
+    // j + DEPTH, stages the x of step j + 1 and asks for that of step j + 1 + DEPTH.
     auto step = [&](int b, int par) {
-        const int buf = WN == 1 ? 0 : par;
+        const int buf = WN == 1 ? 0 : par % 2, next = (par + 1) % DEPTH;
         u32x4 cc[NT];
         u32x2 cs[NT][GPB];
 #pragma unroll
@@ -106,7 +117,7 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
 #pragma unroll
             for (int g = 0; g < GPB; ++g) cs[t][g] = sc[par][t][g];
         }
-        load_codes(b + 2 * WK, c[par], sc[par]);
+        load_codes(b + DEPTH * WK, c[par], sc[par]);
         if (b < L.blocks) {
             const u32x4 *xb = xs + buf * STAGE + slot * MT * 256;
 #pragma unroll
@@ -139,22 +150,24 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
             }
         }
         if constexpr (WN == 1) wave_lds_fence();   // x is this wave's own: LDS serves it in order
-        if (b + WK < L.blocks) stage(buf ^ (WN == 1 ? 0 : 1), xv[par ^ 1]);
-        load_x(b + 3 * WK, xv[par ^ 1]);
+        if (b + WK < L.blocks) stage(buf ^ (WN == 1 ? 0 : 1), xv[next]);
+        load_x(b + (DEPTH + 1) * WK, xv[next]);
         if constexpr (WN == 1) wave_lds_fence();
         else __syncthreads();
     };
-    load_x(slot, xv[0]);
-    load_codes(slot, c[0], sc[0]);
-    load_x(slot + WK, xv[1]);
-    load_codes(slot + WK, c[1], sc[1]);
+#pragma unroll
+    for (int p = 0; p < DEPTH; ++p) {
+        load_x(slot + p * WK, xv[p]);
+        load_codes(slot + p * WK, c[p], sc[p]);
+    }
     if (slot < L.blocks) stage(0, xv[0]);
-    load_x(slot + 2 * WK, xv[0]);
+    load_x(slot + DEPTH * WK, xv[0]);
     if constexpr (WN == 1) wave_lds_fence();
     else __syncthreads();
-    for (int b0 = 0; b0 < L.blocks; b0 += 2 * WK) {
-        step(b0 + slot, 0);
-        if (b0 + WK < L.blocks) step(b0 + WK + slot, 1);
+    for (int b0 = 0; b0 < L.blocks; b0 += DEPTH * WK) {
+#pragma unroll
+        for (int p = 0; p < DEPTH; ++p)
+            if (b0 + p * WK < L.blocks) step(b0 + p * WK + slot, p);
     }
     __syncthreads();
     // The slots' sums, RT tiles at a time, over the staging area.
