@@ -217,36 +217,39 @@ hipError_t launch_linear_dt(const LinearArgs &a, hipStream_t s) {
     return (gpb == 4 ? (tail ? run_linear<DT, NT_, RG_, WN_, 4, true>(a, s) : run_linear<DT, NT_, RG_, WN_, 4, false>(a, s))                      \
      : gpb == 2 ? (tail ? run_linear<DT, NT_, RG_, WN_, 2, true>(a, s) : run_linear<DT, NT_, RG_, WN_, 2, false>(a, s))                    \
                 : run_linear<DT, NT_, RG_, WN_, 1, false>(a, s))
-    // Outputs per workgroup (16 NT WN): the fewest of 16, 32, 64, 128 that leave at most one
-    // workgroup per CU, as each reads all of x again (in us, 32 rows, with 16 / 32 / 64 / 128:
-    // 4096 x 4096 9.1 / 10.2 / 12.7 / 18.8, 8192 x 8192 24.2 / 16.4 / 20.7 / 32.7, 14336 x 4096
-    // 28.3 / 19.4 / 13.4 / 19.5, 28672 x 8192 79.0 / 56.6 / 40.7 / 36.2).  Up to 8 rows read little
-    // of it, and 32 outputs serve every n above (28672 x 8192, one row: 26.4 / 24.8 / 27.0); up
-    // to 16 rows 64 do.  Two waves share the x of 64 rows where 16 outputs a wave would do, as
-    // it fills the registers of one (8192 x 8192, 32 outputs: 25.0, by one wave of 2 tiles 70.9).
+    // Outputs per workgroup (16 NT WN): the fewest that leave at most one workgroup per CU, as
+    // each reads all of x again and a second one on some CUs leaves the others idle (in us, 32
+    // rows, with 16 / 32 / 64 / 128: 4096 x 4096 8.6 / 10.2 / 12.7 / 18.8, 8192 x 8192 24.2 /
+    // 16.4 / 20.7 / 32.7, 14336 x 4096 28.3 / 19.4 / 13.4 / 19.5, 28672 x 8192 79 / 57 / 41 / 38;
+    // 7 rows, 9973 x 3456, with 32 / 48 / 64: 10.3 / 7.6 / 8.5).  Up to 8 rows read little of x,
+    // and 32 outputs serve every n above (28672 x 8192, one row, with 16 / 32 / 64: 26.4 / 24.6 /
+    // 27.0).  Two waves share the x of 64 rows where 16 outputs a wave would do, as it fills the
+    // registers of one (8192 x 8192, 32 outputs: 25.0, by one wave of 2 tiles 70.9).
     const int cus = 256;
-    const int r = n <= 16 * cus ? 16 : n <= 32 * cus ? 32 : n <= 64 * cus ? 64 : 128;
     if (batch <= 4) {
-        if (r == 16) LINEAR(1, 1, 1);
+        if (n <= 16 * cus) LINEAR(1, 1, 1);
+        if (n > 32 * cus && n <= 48 * cus) LINEAR(3, 1, 1);
         LINEAR(2, 1, 1);
     }
     if (batch <= 8) {
-        if (r == 16) LINEAR(1, 2, 1);
+        if (n <= 16 * cus) LINEAR(1, 2, 1);
+        if (n > 32 * cus && n <= 48 * cus) LINEAR(3, 2, 1);
         LINEAR(2, 2, 1);
     }
     if (batch <= 16) {
-        if (r == 16) LINEAR(1, 4, 1);
-        if (r == 32) LINEAR(2, 4, 1);
+        if (n <= 16 * cus) LINEAR(1, 4, 1);
+        if (n <= 32 * cus) LINEAR(2, 4, 1);
+        if (n <= 48 * cus) LINEAR(3, 4, 1);
         LINEAR(4, 4, 1);
     }
     if (batch <= 32) {
-        if (r == 16) LINEAR(1, 8, 1);
-        if (r == 32) LINEAR(2, 8, 1);
-        if (r == 64) LINEAR(2, 8, 2);
+        if (n <= 16 * cus) LINEAR(1, 8, 1);
+        if (n <= 32 * cus) LINEAR(2, 8, 1);
+        if (n <= 64 * cus) LINEAR(2, 8, 2);
         LINEAR(2, 8, 4);
     }
-    if (r <= 32) LINEAR(1, 16, 2);
-    if (r == 64) LINEAR(2, 16, 2);
+    if (n <= 32 * cus) LINEAR(1, 16, 2);
+    if (n <= 64 * cus) LINEAR(2, 16, 2);
     LINEAR(2, 16, 4);
 #undef LINEAR
 }
