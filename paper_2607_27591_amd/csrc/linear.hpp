@@ -41,7 +41,7 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
     extern __shared__ __align__(16) unsigned char smem[];
     u32x4 *xs = reinterpret_cast<u32x4 *>(smem);
     const LinearLayout L(A.n, A.k, A.group);
-    const int batch = A.batch, n = A.n, k = A.k;
+    const int n = A.n, k = A.k, row0 = blockIdx.y * 4 * RG, batch = min(A.batch - row0, 4 * RG);   // rows of this workgroup
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int lane = lane_id(), h = lane / 16, col = lane % 16;
     const int slot = wave / WN, nw = wave % WN;
@@ -52,7 +52,7 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
     // last row again (their columns are not stored).
     const uint16_t *xr[XL];
 #pragma unroll
-    for (int l = 0; l < XL; ++l) xr[l] = A.x + (size_t)min(4 * (nw * XL + l) + h, batch - 1) * A.ldx + 8 * col;
+    for (int l = 0; l < XL; ++l) xr[l] = A.x + (size_t)(row0 + min(4 * (nw * XL + l) + h, batch - 1)) * A.ldx + 8 * col;
     const uint8_t *codes[NT];
     const uint16_t *scales[NT];
 #pragma unroll
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
             const int t = (r + u) / MT, b = 16 * ((r + u) % MT) + col;
             const int j = (tile0 + t) * kLinearRows + 4 * h;
             if (b < batch) {
-                uint16_t *dst = A.y + (size_t)b * A.ldy;
+                uint16_t *dst = A.y + (size_t)(row0 + b) * A.ldy;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (j + e < n) dst[j + e] = float_to_half<DT>(s[e] + (A.bias ? half_to_float<DT>(A.bias[j + e]) : 0.0f));
@@ -204,7 +204,8 @@ static hipError_t run_linear(const LinearArgs &a, hipStream_t s) {
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
     }
-    kernel<<<(unsigned)((a.n + R - 1) / R), 64 * kLinearWaves, lds, s>>>(a);
+    const dim3 grid((unsigned)((a.n + R - 1) / R), (unsigned)((a.batch + 4 * RG - 1) / (4 * RG)));
+    kernel<<<grid, 64 * kLinearWaves, lds, s>>>(a);
     return hipGetLastError();
 }
 
@@ -217,39 +218,45 @@ hipError_t launch_linear_dt(const LinearArgs &a, hipStream_t s) {
     return (gpb == 4 ? (tail ? run_linear<DT, NT_, RG_, WN_, 4, true>(a, s) : run_linear<DT, NT_, RG_, WN_, 4, false>(a, s))                      \
      : gpb == 2 ? (tail ? run_linear<DT, NT_, RG_, WN_, 2, true>(a, s) : run_linear<DT, NT_, RG_, WN_, 2, false>(a, s))                    \
                 : run_linear<DT, NT_, RG_, WN_, 1, false>(a, s))
-    // Outputs per workgroup (16 NT WN): the fewest that leave at most one workgroup per CU, as
-    // each reads all of x again and a second one on some CUs leaves the others idle (in us, 32
-    // rows, with 16 / 32 / 64 / 128: 4096 x 4096 8.6 / 10.2 / 12.7 / 18.8, 8192 x 8192 24.2 /
-    // 16.4 / 20.7 / 32.7, 14336 x 4096 28.3 / 19.4 / 13.4 / 19.5, 28672 x 8192 79 / 57 / 41 / 38;
-    // 7 rows, 9973 x 3456, with 32 / 48 / 64: 10.3 / 7.6 / 8.5).  Up to 8 rows read little of x,
-    // and 32 outputs serve every n above (28672 x 8192, one row, with 16 / 32 / 64: 26.4 / 24.6 /
-    // 27.0).  Two waves share the x of 64 rows where 16 outputs a wave would do, as it fills the
-    // registers of one (8192 x 8192, 32 outputs: 25.0, by one wave of 2 tiles 70.9).
+    // Outputs (16 NT WN) and rows (4 RG) per workgroup: the variant that reads least (codes once
+    // per row tile, x once per group of outputs) among those with at most one workgroup per CU, as
+    // a second one on some CUs leaves the others idle.  In us, by outputs x rows:
+    //   7 rows    9973 x 3456   32: 10.3, 48: 7.6, 64: 8.5
+    //   32 rows   1024 x 4096   16 x 16: 5.0, 16 x 32: 6.9      4096 x 4096  32 x 16: 7.4, 16 x 32: 8.8
+    //             8192 x 8192   32 x 32: 16.1, 64 x 32: 21.9    14336 x 4096 64 x 32: 14.2, 128 x 32: 20.8
+    //             28672 x 8192  32 x 32: 55, 64 x 32: 43, 128 x 32: 40
+    //   64 rows   1024 x 4096   16 x 16: 6.0, 32 x 16: 7.1, 32 x 64: 15.4
+    //             4096 x 4096   64 x 16: 9.8, 32 x 32: 10.1, 32 x 64: 15.6
+    //             8192 x 8192   64 x 32: 22.1, 32 x 64: 25.8    14336 x 4096 64 x 64: 20.9, 64 x 32: 25.8
+    //             28672 x 8192  64 x 64: 78, 128 x 64: 55
+    // Up to 8 rows read little of x, and 32 outputs serve every n above (28672 x 8192, one row,
+    // with 16 / 32 / 64: 26.4 / 24.6 / 27.0).
     const int cus = 256;
+    auto fits = [&](int outputs, int rows) { return (n + outputs - 1) / outputs * ((batch + rows - 1) / rows) <= cus; };
     if (batch <= 4) {
-        if (n <= 16 * cus) LINEAR(1, 1, 1);
-        if (n > 32 * cus && n <= 48 * cus) LINEAR(3, 1, 1);
+        if (fits(16, 4)) LINEAR(1, 1, 1);
+        if (!fits(32, 4) && fits(48, 4)) LINEAR(3, 1, 1);
         LINEAR(2, 1, 1);
     }
     if (batch <= 8) {
-        if (n <= 16 * cus) LINEAR(1, 2, 1);
-        if (n > 32 * cus && n <= 48 * cus) LINEAR(3, 2, 1);
+        if (fits(16, 8)) LINEAR(1, 2, 1);
+        if (!fits(32, 8) && fits(48, 8)) LINEAR(3, 2, 1);
         LINEAR(2, 2, 1);
     }
+    if (fits(16, 16)) LINEAR(1, 4, 1);
+    if (fits(32, 16)) LINEAR(2, 4, 1);
     if (batch <= 16) {
-        if (n <= 16 * cus) LINEAR(1, 4, 1);
-        if (n <= 32 * cus) LINEAR(2, 4, 1);
-        if (n <= 48 * cus) LINEAR(3, 4, 1);
+        if (fits(48, 16)) LINEAR(3, 4, 1);
         LINEAR(4, 4, 1);
     }
     if (batch <= 32) {
-        if (n <= 16 * cus) LINEAR(1, 8, 1);
-        if (n <= 32 * cus) LINEAR(2, 8, 1);
-        if (n <= 64 * cus) LINEAR(2, 8, 2);
+        if (fits(32, 32)) LINEAR(2, 8, 1);
+        if (fits(64, 32)) LINEAR(2, 8, 2);
         LINEAR(2, 8, 4);
     }
-    if (n <= 32 * cus) LINEAR(1, 16, 2);
-    if (n <= 64 * cus) LINEAR(2, 16, 2);
+    if (fits(64, 16)) LINEAR(4, 4, 1);
+    if (fits(64, 32)) LINEAR(2, 8, 2);
+    if (fits(64, 64)) LINEAR(2, 16, 2);
     LINEAR(2, 16, 4);
 #undef LINEAR
 }

@@ -58,6 +58,17 @@ def test_parity(n, k, group, batch, dtype, bias):
     assert torch.equal(y, prox.linear_w4(q, x, bias=b))   # the same bits every time
 
 
+# Outputs and rows on both sides of every size at which a call takes another variant.
+EDGES = [(n, b) for n in (1024, 1025, 2048, 4096, 4097, 8192, 8193, 12288, 12290, 16384, 16390) for b in (1, 8, 16, 17, 32, 33, 64)]
+
+
+@pytest.mark.parametrize("n,batch", EDGES)
+def test_variants(n, batch):
+    group, k, dtype = [(32, 224, BF16), (64, 320, F16), (128, 384, BF16), (128, 256, F16)][(n + batch) % 4]
+    q, codes, scales = _case(n, k, group, dtype, seed=n)
+    _check(q, codes, scales, _randn((batch, k), 1, dtype), _randn((n,), 2, dtype), f"{n}x{k} g{group} b{batch}")
+
+
 @pytest.mark.parametrize("dtype,lo,hi", [(BF16, 1e-30, 1e30), (F16, 6e-8, 6e4)])
 @pytest.mark.parametrize("batch", [1, 5, 40])
 def test_inputs_of_any_size(dtype, lo, hi, batch):
