@@ -34,7 +34,7 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs &A, const SeqTokens
 // Waves per SIMD that the registers of a variant allow without spilling.
 constexpr int attn_waves(int D, int NG, int QT) {
     if (QT == 1) return D == 64 ? 5 : D == 128 ? (NG == 4 ? 3 : 4) : (NG == 2 ? 3 : 2);
-    return D == 64 ? (NG == 1 ? 4 : 3) : D == 128 ? (NG == 1 ? 3 : 2) : 1;
+    return D == 64 ? (NG == 1 ? 3 : 2) : D == 128 ? (NG == 1 ? 3 : 2) : 1;
 }
 
 // A lane's W words of a half block of keys or a block of values (kv_k_word, kv_v_word).
@@ -94,6 +94,197 @@ __device__ __forceinline__ size_t attn_part_row(const AttnArgs &A, int split, in
     return ((((size_t)split * A.s.n_seq + s) * A.c.heads + head) * A.tiles + tile) * A.part_rows;
 }
 
+// What a wave keeps of QT tiles of 16 query rows (row l % 16 in lane l) during its pass:
+// the unnormalised output and the offset's part of it, maximum m of scale times the score,
+// the lane's part of the sum of weights l; a score above top raises m.
+template <int D, int NG, int QT>
+struct AttnRows {
+    static constexpr int VT = D / 16, VPG = VT / NG;
+    v4f acc[QT][VT], off[QT][NG];
+    float m[QT], l[QT], top[QT];
+    int lo[QT], hi[QT];                    // positions that the row sees
+    int hi_min, hi_max, lo_min, lo_max;    // over the tiles' rows
+
+    // Rows r0 .. r1 of the sequence and kv head (the last one again past them).
+    __device__ __forceinline__ void start(const AttnArgs &A, const SeqTokens &sq, int r0, int r1) {
+        const int i0 = r0 / A.ratio, i1 = r1 / A.ratio, col = lane_id() % 16;
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            hi[u] = sq.pos0 + min(r0 + 16 * u + col, r1) / A.ratio;
+            lo[u] = A.window > 0 ? hi[u] - A.window + 1 : 0;
+            m[u] = top[u] = kAttnNone;
+            l[u] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VT; ++i) acc[u][i] = v4f{0, 0, 0, 0};
+#pragma unroll
+            for (int g = 0; g < NG; ++g) off[u][g] = v4f{0, 0, 0, 0};
+        }
+        hi_min = sq.pos0 + i0;
+        hi_max = sq.pos0 + i1;
+        lo_min = A.window > 0 ? hi_min - A.window + 1 : 0;
+        lo_max = A.window > 0 ? hi_max - A.window + 1 : 0;
+    }
+    // Whether some row does not see all of the block at p0.
+    __device__ __forceinline__ bool edge(int p0) const { return p0 + kKvBlock - 1 > hi_min || p0 < lo_max; }
+
+    // Scores of the block at p0 to weights, the sums raised to a new maximum where it takes one.
+    __device__ __forceinline__ void weigh(float (&sc)[QT][2][4], int p0, bool edge, float scale, float slack) {
+        const int h = lane_id() / 16;
+        uint32_t seen[QT];   // bit 4 j + e: the row sees the token
+        bool up = false;
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            float mx = kAttnNone;
+            if (edge) {
+                seen[u] = 0;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int p = p0 + 16 * j + 4 * h + e;
+                        const bool ok = p <= hi[u] && p >= lo[u];
+                        seen[u] |= (uint32_t)ok << (4 * j + e);
+                        sc[u][j][e] = ok ? sc[u][j][e] : kAttnNone;   // whatever stands there
+                    }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[u][j][e]);
+            up |= mx > top[u];
+        }
+        if (__any(up)) {
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                float mx = kAttnNone;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[u][j][e]);
+                mx = max_swap32(max_swap16(mx));
+                const float m2 = fmaxf(m[u], mx * scale), f = __builtin_amdgcn_exp2f(m[u] - m2);
+                top[u] = fmaxf(top[u], mx + slack);
+                m[u] = m2;
+                l[u] *= f;
+#pragma unroll
+                for (int i = 0; i < VT; ++i) acc[u][i] *= f;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) off[u][g] *= f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float p = __builtin_amdgcn_exp2f(fmaf(sc[u][j][e], scale, -m[u]));
+                    if (edge) p = (seen[u] >> (4 * j + e)) & 1 ? p : 0.0f;
+                    sc[u][j][e] = p;
+                    l[u] += p;
+                }
+    }
+
+    // Weights times values: value(i) is the operand of channels 16 i .. 16 i + 15, vs their scales.
+    template <typename Value>
+    __device__ __forceinline__ void add(const float (&p)[QT][2][4], const u32x4 (&vs)[NG], int p0, bool edge,
+                                        const Bf16Left &left, Value value) {
+        const int h = lane_id() / 16;
+        const uint4 minus = Int4Oct<kBF16>::minus();
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            uint4 ph[QT], pl[QT];
+            float f[2][4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    f[j][e] = slot_scale(vs[g], j, e);
+                    if (edge) {   // tokens that no row sees may hold anything
+                        const int q = p0 + 16 * j + 4 * h + e;
+                        f[j][e] = q <= hi_max && q >= lo_min ? f[j][e] : 0.0f;
+                    }
+                }
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                uint32_t wh[4], wl[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = times(p[u][0][e], f[0][e]), c = times(p[u][1][e], f[1][e]);
+                    wh[e] = pack_bf16(a, c);
+                    wl[e] = pack_bf16(left.minus_lo(a, wh[e]), left.minus_hi(c, wh[e]));
+                }
+                ph[u] = make_uint4(wh[0], wh[1], wh[2], wh[3]);
+                pl[u] = make_uint4(wl[0], wl[1], wl[2], wl[3]);
+                off[u][g] = mfma32<kBF16>(minus, ph[u], off[u][g]);
+                off[u][g] = mfma32<kBF16>(minus, pl[u], off[u][g]);
+            }
+#pragma unroll
+            for (int i = g * VPG; i < (g + 1) * VPG; ++i) {
+                const uint4 a = value(i);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) acc[u][i] = mfma32<kBF16>(a, ph[u], acc[u][i]);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) acc[u][i] = mfma32<kBF16>(a, pl[u], acc[u][i]);
+            }
+        }
+    }
+
+    // The offset's part comes off, before it can outgrow the sums.
+    __device__ __forceinline__ void flush() {
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+#pragma unroll
+                for (int i = g * VPG; i < (g + 1) * VPG; ++i) acc[u][i] += off[u][g];
+                off[u][g] = v4f{0, 0, 0, 0};
+            }
+    }
+};
+
+// Scores of two half blocks of 16 tokens: sums of a group, base its start (the offset's part), its scales applied.
+template <int NG, int QT>
+__device__ __forceinline__ void add_scores(float (&sc)[QT][2][4], const v4f (&d)[QT][2], const u32x4 &ks, int g) {
+#pragma unroll
+    for (int u = 0; u < QT; ++u)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float f = slot_scale(ks, j, e);
+                sc[u][j][e] = g == 0 ? times(d[u][j][e], f) : fmaf(d[u][j][e], f, sc[u][j][e]);
+            }
+}
+
+// Query row r of a sequence and kv head as an operand: word w of the lane.
+template <int D>
+__device__ __forceinline__ uint4 query_word(const AttnArgs &A, const SeqTokens &sq, int head, int r, int w) {
+    const int i = r / A.ratio;
+    const uint16_t *p = A.q + (size_t)(sq.t0 + i) * A.ldq + (size_t)(head * A.ratio + r - i * A.ratio) * D + 8 * (lane_id() / 16);
+    const uint4 v = *reinterpret_cast<const uint4 *>(p + 32 * w);
+    return make_uint4(v.x ^ A.q_sign, v.y ^ A.q_sign, v.z ^ A.q_sign, v.w ^ A.q_sign);
+}
+
+// Blocks of a sequence and kv head in the cache.
+template <int D, int NG>
+struct AttnBlocks {
+    const int32_t *table;
+    int per, last;   // blocks of a page, the last block
+    __device__ __forceinline__ AttnBlocks(const AttnArgs &A, int s, int end)
+        : table(A.s.table + (size_t)s * A.s.max_pages), per(A.c.page_size / kKvBlock), last(end - 1) {}
+    __device__ __forceinline__ int page_of(const AttnArgs &A, int b) const { return A.page_shift >= 0 ? b >> A.page_shift : b / per; }
+    __device__ __forceinline__ int page_id(const AttnArgs &A, int b) const { return table[page_of(A, min(b, last))]; }
+    // Record of block b on page id; where the page lies outside the cache, or past the end, ok is
+    // false and the cache's first record stands in (loaded, not used).
+    __device__ __forceinline__ const uint8_t *record(const AttnArgs &A, int head, int b, int end, int id, bool &ok) const {
+        const int pid = __builtin_amdgcn_readfirstlane(id);
+        ok = b < end && pid >= 0 && pid < A.c.n_pages;
+        const size_t at = (size_t)pid * A.c.page_bytes + ((size_t)head * per + (b - page_of(A, b) * per)) * KvLayout(D, D / NG).record;
+        return A.c.blob + (ok ? at : 0);
+    }
+};
+
 // One pass over the cache with the running maximum and sum of the softmax.  A wave takes
 // blocks of 32 tokens; with K the codes of 16 tokens and Q 16 query rows of one kv head,
 //   S^T = K Q^T             codes exact with an offset (base starts each group's sum), scales
@@ -101,8 +292,8 @@ __device__ __forceinline__ size_t attn_part_row(const AttnArgs &A, int split, in
 //   P   = 2^(c S - m)       fp32; l += P
 //   O^T += V^T (P sv)^T     P times the values' scale, rounded to two bf16 terms (2^-17), is
 //                           the second product's operand as it stands, no lane exchange; the
-//                           codes' offset comes off with a product of its own (acc_off), before
-//                           it can outgrow the sums (every 8 blocks).
+//                           codes' offset comes off with a product of its own (off), every 8
+//                           blocks.
 // Two terms, as one bf16 term would add as much error as the rounding of a bf16 output, and
 // eight times that of an fp16 one; bf16 and not fp16, as P sv spans any range.
 // Bound by HBM for single tokens (a record is read once and contiguous; the next one's loads
@@ -111,7 +302,7 @@ __device__ __forceinline__ size_t attn_part_row(const AttnArgs &A, int split, in
 // cache by attn_join_kernel.
 template <int DT, int D, int NG, int QT>
 __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_kernel(AttnArgs A) {
-    constexpr int R = 16 * QT, KW = D / 32, VT = D / 16, SPG = KW / NG, VPG = VT / NG;
+    constexpr int R = 16 * QT, KW = D / 32, VT = D / 16, SPG = KW / NG;
     constexpr int TC = VT < 8 ? VT : 8;   // channel tiles joined at a time
     constexpr KvLayout L(D, D / NG);
     // Queries and base as operands during the pass (read again for each block, which leaves
@@ -137,18 +328,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
 
     uint32_t xk[2][KW], xv[VT];
     u32x4 xks[NG], xvs[NG];
-    const int32_t *table = A.s.table + (size_t)s * A.s.max_pages;
-    const int per = A.c.page_size / kKvBlock;
-    auto page_of = [&](int b) { return A.page_shift >= 0 ? b >> A.page_shift : b / per; };
-    auto page_id = [&](int b) { return table[page_of(min(b, sp.b1 - 1))]; };
-    // Record of block b; where its page lies outside the cache, or past the end, ok is false
-    // and the cache's first record stands in (loaded, not used).
-    auto record = [&](int b, int id, bool &ok) {
-        const int pid = __builtin_amdgcn_readfirstlane(id);
-        ok = b < b_end && pid >= 0 && pid < A.c.n_pages;
-        const size_t at = (size_t)pid * A.c.page_bytes + ((size_t)head * per + (b - page_of(b) * per)) * L.record;
-        return A.c.blob + (ok ? at : 0);
-    };
+    const AttnBlocks<D, NG> blocks(A, s, sp.b1);
     auto load_k = [&](const uint8_t *rec) {
         load_words(xk[0], rec, lane);
         load_words(xk[1], rec + 64 * KW * 4, lane);
@@ -167,80 +347,36 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
     bool next_ok = false;
     const uint8_t *next = A.c.blob;
     if (first < b_end) {
-        next = record(first, page_id(first), next_ok);
-        next_id = page_id(first + kAttnWaves);
+        next = blocks.record(A, head, first, b_end, blocks.page_id(A, first), next_ok);
+        next_id = blocks.page_id(A, first + kAttnWaves);
         load_k(next);
         load_v(next);
     }
-    // Queries as operands, and what each lane's row may see.
-    int lo[QT], hi[QT];
-    int lo_max = 0, hi_min = 0x7FFFFFFF;
+    const int r_last = min(r0 + R, rows) - 1;
     const Int4Oct<DT> kop;
     const Int4Oct<kBF16> vop;
     const Bf16Left left;
-    const uint4 kminus = Int4Oct<DT>::minus(), vminus = Int4Oct<kBF16>::minus();
-    const v4f zero{0, 0, 0, 0};
 #pragma unroll
-    for (int u = 0; u < QT; ++u) {
-        const int r = min(r0 + 16 * u + col, rows - 1), i = r / A.ratio;   // past the last row: it again
-        const uint16_t *p = A.q + (size_t)(sq.t0 + i) * A.ldq + (size_t)(head * A.ratio + r - i * A.ratio) * D + 8 * h;
-        for (int w = wave; w < KW; w += kAttnWaves) {
-            uint4 v = *reinterpret_cast<const uint4 *>(p + 32 * w);
-            v.x ^= A.q_sign;
-            v.y ^= A.q_sign;
-            v.z ^= A.q_sign;
-            v.w ^= A.q_sign;
-            smem[u * KW + w][lane] = __builtin_bit_cast(v4f, v);
-        }
-        hi[u] = sq.pos0 + i;
-        lo[u] = A.window > 0 ? hi[u] - A.window + 1 : 0;
-    }
+    for (int u = 0; u < QT; ++u)
+        for (int w = wave; w < KW; w += kAttnWaves)
+            smem[u * KW + w][lane] = __builtin_bit_cast(v4f, query_word<D>(A, sq, head, min(r0 + 16 * u + col, r_last), w));
     __syncthreads();
     for (int ug = wave; ug < QT * NG; ug += kAttnWaves) {
-        v4f d = zero;
+        v4f d{0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < SPG; ++w)
-            d = mfma32<DT>(kminus, __builtin_bit_cast(uint4, smem[ug / NG * KW + ug % NG * SPG + w][lane]), d);
+            d = mfma32<DT>(Int4Oct<DT>::minus(), __builtin_bit_cast(uint4, smem[ug / NG * KW + ug % NG * SPG + w][lane]), d);
         smem[QT * KW + ug][lane] = d;
     }
     __syncthreads();
-    {   // over the tile's rows, from its first and last
-        const int i0 = r0 / A.ratio, i1 = (min(r0 + R, rows) - 1) / A.ratio;
-        hi_min = sq.pos0 + i0;
-        lo_max = A.window > 0 ? sq.pos0 + i1 - A.window + 1 : 0;
-    }
-    const int hi_max = sq.pos0 + (min(r0 + R, rows) - 1) / A.ratio;
-    const int lo_min = A.window > 0 ? hi_min - A.window + 1 : 0;
-
-    v4f acc[QT][VT], acc_off[QT][NG];
-    // Running maximum m of scale times the score; a score above top raises it.
-    float m[QT], l[QT], top[QT];
+    AttnRows<D, NG, QT> X;
+    X.start(A, sq, r0, r_last);
     const float slack = kAttnSlack / A.scale;
-#pragma unroll
-    for (int u = 0; u < QT; ++u) {
-        m[u] = top[u] = kAttnNone;
-        l[u] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < VT; ++i) acc[u][i] = zero;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) acc_off[u][g] = zero;
-    }
-
-    auto flush = [&] {
-#pragma unroll
-        for (int u = 0; u < QT; ++u)
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-#pragma unroll
-                for (int i = g * VPG; i < (g + 1) * VPG; ++i) acc[u][i] += acc_off[u][g];
-                acc_off[u][g] = zero;
-            }
-    };
     int done = 0;
     for (int b = first; b < b_end; b += kAttnWaves) {
         const bool ok = next_ok;
-        next = record(b + kAttnWaves, next_id, next_ok);
-        next_id = page_id(b + 2 * kAttnWaves);
+        next = blocks.record(A, head, b + kAttnWaves, b_end, next_id, next_ok);
+        next_id = blocks.page_id(A, b + 2 * kAttnWaves);
         float sc[QT][2][4];
         if (ok) {
             asm volatile("" ::: "memory");   // the queries stay in LDS
@@ -261,116 +397,19 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
                         for (int u = 0; u < QT; ++u) d[u][j] = mfma32<DT>(a, q[u], d[u][j]);
                     }
                 }
-#pragma unroll
-                for (int u = 0; u < QT; ++u)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float f = slot_scale(xks[g], j, e);
-                            sc[u][j][e] = g == 0 ? times(d[u][j][e], f) : fmaf(d[u][j][e], f, sc[u][j][e]);
-                        }
+                add_scores<NG, QT>(sc, d, xks[g], g);
             }
         }
         load_k(next);
         if (ok) {
-        const int p0 = b * kKvBlock;
-        const bool edge = p0 + kKvBlock - 1 > hi_min || p0 < lo_max;   // some row does not see all of it
-        uint32_t seen[QT];   // bit 4 j + e: the row sees the token
-        bool up = false;
-#pragma unroll
-        for (int u = 0; u < QT; ++u) {
-            float mx = kAttnNone;
-            if (edge) {
-                seen[u] = 0;
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int p = p0 + 16 * j + 4 * h + e;
-                        const bool ok2 = p <= hi[u] && p >= lo[u];
-                        seen[u] |= (uint32_t)ok2 << (4 * j + e);
-                        sc[u][j][e] = ok2 ? sc[u][j][e] : kAttnNone;   // whatever stands there
-                    }
-            }
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[u][j][e]);
-            up |= mx > top[u];
-        }
-        if (__any(up)) {
-#pragma unroll
-            for (int u = 0; u < QT; ++u) {
-                float mx = kAttnNone;
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[u][j][e]);
-                mx = max_swap32(max_swap16(mx));
-                const float m2 = fmaxf(m[u], mx * A.scale), f = __builtin_amdgcn_exp2f(m[u] - m2);
-                top[u] = fmaxf(top[u], mx + slack);
-                m[u] = m2;
-                l[u] *= f;
-#pragma unroll
-                for (int i = 0; i < VT; ++i) acc[u][i] *= f;
-#pragma unroll
-                for (int g = 0; g < NG; ++g) acc_off[u][g] *= f;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < QT; ++u)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float p = __builtin_amdgcn_exp2f(fmaf(sc[u][j][e], A.scale, -m[u]));
-                    if (edge) p = (seen[u] >> (4 * j + e)) & 1 ? p : 0.0f;
-                    sc[u][j][e] = p;
-                    l[u] += p;
-                }
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            uint4 ph[QT], pl[QT];
-            float f[2][4];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    f[j][e] = slot_scale(xvs[g], j, e);
-                    if (edge) {   // tokens that no row sees may hold anything
-                        const int p = p0 + 16 * j + 4 * h + e;
-                        f[j][e] = p <= hi_max && p >= lo_min ? f[j][e] : 0.0f;
-                    }
-                }
-#pragma unroll
-            for (int u = 0; u < QT; ++u) {
-                uint32_t wh[4], wl[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float a = times(sc[u][0][e], f[0][e]), c = times(sc[u][1][e], f[1][e]);
-                    wh[e] = pack_bf16(a, c);
-                    wl[e] = pack_bf16(left.minus_lo(a, wh[e]), left.minus_hi(c, wh[e]));
-                }
-                ph[u] = make_uint4(wh[0], wh[1], wh[2], wh[3]);
-                pl[u] = make_uint4(wl[0], wl[1], wl[2], wl[3]);
-                acc_off[u][g] = mfma32<kBF16>(vminus, ph[u], acc_off[u][g]);
-                acc_off[u][g] = mfma32<kBF16>(vminus, pl[u], acc_off[u][g]);
-            }
-#pragma unroll
-            for (int i = g * VPG; i < (g + 1) * VPG; ++i) {
-                const uint4 a = vop(xv[i]);
-#pragma unroll
-                for (int u = 0; u < QT; ++u) acc[u][i] = mfma32<kBF16>(a, ph[u], acc[u][i]);
-#pragma unroll
-                for (int u = 0; u < QT; ++u) acc[u][i] = mfma32<kBF16>(a, pl[u], acc[u][i]);
-            }
-        }
-        if ((++done & 7) == 0) flush();
+            const bool edge = X.edge(b * kKvBlock);
+            X.weigh(sc, b * kKvBlock, edge, A.scale, slack);
+            X.add(sc, xvs, b * kKvBlock, edge, left, [&](int i) { return vop(xv[i]); });
+            if ((++done & 7) == 0) X.flush();
         }
         load_v(next);
     }
-    flush();
+    X.flush();
 
     // The waves' results: o = sum_w 2^(m_w - m) o_w, l alike, in a fixed order.
     float *part_o = reinterpret_cast<float *>(A.ws);
@@ -378,10 +417,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
     const size_t prow = attn_part_row(A, split, s, head, tile);
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
-        const float lw = add_swap32(add_swap16(l[u]));
+        const float lw = add_swap32(add_swap16(X.l[u]));
         if (u > 0) __syncthreads();
         if (h == 0) {
-            m_sh[wave][col] = m[u];
+            m_sh[wave][col] = X.m[u];
             l_sh[wave][col] = lw;
         }
         __syncthreads();
@@ -390,7 +429,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
         for (int w = 1; w < kAttnWaves; ++w) mm = fmaxf(mm, m_sh[w][col]);
 #pragma unroll
         for (int w = 0; w < kAttnWaves; ++w) ll = fmaf(l_sh[w][col], __builtin_amdgcn_exp2f(m_sh[w][col] - mm), ll);
-        const float f = __builtin_amdgcn_exp2f(m[u] - mm);
+        const float f = __builtin_amdgcn_exp2f(X.m[u] - mm);
         const int r = r0 + 16 * u + col, i = r / A.ratio;
         uint16_t *dst = A.out + (size_t)(sq.t0 + i) * A.ldo + (size_t)(head * A.ratio + r - i * A.ratio) * D + 4 * h;
         const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
@@ -399,7 +438,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
         for (int c = 0; c < VT; c += TC) {
             if (c > 0) __syncthreads();
 #pragma unroll
-            for (int i2 = 0; i2 < TC; ++i2) o_sh[wave * TC + i2][lane] = acc[u][c + i2] * f;
+            for (int i2 = 0; i2 < TC; ++i2) o_sh[wave * TC + i2][lane] = X.acc[u][c + i2] * f;
             __syncthreads();
             for (int i2 = wave; i2 < TC; i2 += kAttnWaves) {
                 v4f o = o_sh[i2][lane];

@@ -68,6 +68,12 @@ SHAPES = [  # heads, ratio, dim, group, page, dtype, lengths, new tokens, window
     (1, 64, 64, 32, 64, BF16, [100, 63], [2, 1], 0),
     (2, 4, 128, 64, 64, F16, [20000], [1], 0),
     (1, 8, 128, 32, 256, BF16, [9001, 3, 5000], [2, 1, 1], 0),
+    # many rows of many heads: the cache is not split
+    (8, 1, 128, 64, 64, BF16, [300] * 16, [70] * 16, 0),
+    (16, 2, 64, 32, 32, F16, [150, 90, 400, 33, 70, 64, 100, 65], [90, 90, 130, 1, 70, 64, 3, 65], 0),
+    (16, 3, 64, 64, 96, BF16, [260, 130, 95, 30], [200, 128, 95, 40], 50),
+    (32, 4, 128, 128, 128, F16, [100, 64], [100, 64], 0),
+    (32, 1, 128, 32, 32, BF16, [333, 200], [200, 140], 33),
 ]
 
 
