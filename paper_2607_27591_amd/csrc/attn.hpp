@@ -9,6 +9,7 @@ namespace prox {
 
 constexpr int kAttnWaves = 4;
 constexpr int kAttnMinBlocks = 4;      // blocks of 32 tokens per workgroup, before the cache is split
+constexpr int kAttnWhole = 16;         // ... that are never split
 constexpr float kAttnNone = -3.0e38f;  // running maximum before the first score (finite: no inf - inf)
 // The running maximum m of a row's scores (log2) is raised only when a score exceeds it by more
 // than this: weights stay below 2^8, and sums and outputs are rescaled a few times in all.
@@ -528,11 +529,16 @@ hipError_t run_attn(AttnArgs &a, hipStream_t s) {
     a.tiles = (int)(((long long)a.s.max_new * a.ratio + R - 1) / R);
     // Splits: as many workgroups as the chip holds at a time, one wave of each on a SIMD, no
     // shorter than kAttnMinBlocks, as far as the partial results fit their area (twice as many,
-    // in us: 32 x 8192 tokens 41.8 instead of 40.3, 131072 tokens 41.5 instead of 37.5).
+    // in us: 32 x 8192 tokens 41.8 instead of 40.3, 131072 tokens 41.5 instead of 37.5).  Up to
+    // kAttnWhole blocks are left whole: joining takes longer than the blocks (one launch more).
     const long long base = (long long)a.s.n_seq * a.c.heads * a.tiles;
-    const int blocks = (a.s.max_kv + kKvBlock - 1) / kKvBlock;
+    int blocks = (a.s.max_kv + kKvBlock - 1) / kKvBlock;
+    if (a.window > 0) {   // what the rows of a tile see at most
+        const long long seen = ((long long)a.window + R / a.ratio + 2 * kKvBlock) / kKvBlock;
+        if (seen < blocks) blocks = (int)seen;
+    }
     const long long target = 256 * attn_waves(D, NG, QT);
-    long long n = target / base;
+    long long n = blocks > kAttnWhole ? target / base : 1;
     if (n > kAttnMaxSplits) n = kAttnMaxSplits;
     a.part_rows = (int)((long long)a.s.max_new * a.ratio < R ? a.s.max_new * a.ratio : R);
     if (n > kAttnPartRows / a.part_rows / base) n = kAttnPartRows / a.part_rows / base;
