@@ -480,8 +480,12 @@ size_t prox_kv_bytes(int kv_heads, int head_dim, int group, int page_size, int n
  *              left as they are
  *   page_table a position whose entry lies outside [0, n_pages) is not stored,
  *              reads as 0 and is hidden from attention
- * Two sequences may share pages that a call only reads; pages that a call
- * appends to must belong to one sequence.
+ * Two sequences may share pages that a call only reads; a page that a call
+ * appends to must belong to one sequence and stand once in its row.
+ * The grid covers max_new rows of every sequence: a call that would take more
+ * than 2^23 workgroups is PROX_ERR_UNSUPPORTED.  Attention takes n_seq * kv_heads *
+ * ceil(max_new * q_heads / kv_heads / 16) at most, an append n_seq * kv_heads *
+ * ceil((max_new + 31) / 32) and n_seq * max_new * q_heads * head_dim / 2048.
  */
 typedef struct {
     int n_seq;                   /* 1 .. 65536 */
@@ -539,7 +543,8 @@ prox_status prox_kv_read(const prox_kv_cache *c, const prox_kv_seqs *s, float *k
  * see no position, get 0.
  *   q, out  device, token t's head h at q + t * ldq + h * head_dim (16-byte aligned;
  *           ldq, ldo multiples of 8, >= q_heads * head_dim); out may be q with ldo = ldq
- *   q_heads a multiple of kv_heads
+ *   q_heads a multiple of kv_heads, at most 4096
+ *   scale   any sign; scale / ln 2 must be a finite fp32 number
  *   ws      device, 256-byte aligned, ws_bytes >= prox_kv_attn_workspace_bytes(),
  *           one size for every call with this head_dim; needs no initialisation
  * Results are the same for every run, and depend on max_kv and max_new only in

@@ -2,6 +2,7 @@
 // validation on the host, then one launch each.
 #include <prox.h>
 
+#include <cfloat>
 #include <cmath>
 
 #include "kernels.hpp"
@@ -158,17 +159,19 @@ prox_status prox_kv_attn(const prox_kv_cache *c, const prox_kv_seqs *s, const vo
     if (st != PROX_OK) return st;
     st = check_seqs(s, c, &ks);
     if (st != PROX_OK) return st;
-    if (q_heads < 1 || q_heads > 4096 || q_heads % kc.heads != 0 || window < 0 || !std::isfinite(scale)) return PROX_ERR_INVALID;
+    if (q_heads < 1 || q_heads > 4096 || q_heads % kc.heads != 0 || window < 0) return PROX_ERR_INVALID;
+    const double scale2 = std::fabs((double)scale) * 1.4426950408889634;   // of powers of 2
+    if (!(scale2 <= FLT_MAX)) return PROX_ERR_INVALID;
     if (!ws || !aligned(ws, 256)) return PROX_ERR_INVALID;
     if (ws_bytes < attn_workspace_bytes(kc.dim)) return PROX_ERR_WORKSPACE;
     if (ks.n_tokens == 0) return PROX_OK;
     if (!rows_ok(q, ldq, q_heads, kc.dim) || !rows_ok(out, ldo, q_heads, kc.dim) || (q == out && ldq != ldo))
         return PROX_ERR_INVALID;
-    if ((long long)ks.n_seq * ks.max_new * q_heads > kMaxGrid) return PROX_ERR_UNSUPPORTED;
+    const int ratio = q_heads / kc.heads;   // at least 16 rows a workgroup (a split grid is small)
+    if (ks.n_seq * (((long long)ks.max_new * ratio + 15) / 16) * kc.heads > kMaxGrid) return PROX_ERR_UNSUPPORTED;
     const int per = kc.page_size / kKvBlock;
     AttnArgs a{kc, ks, static_cast<const uint16_t *>(q), static_cast<uint16_t *>(out), ldq, ldo, q_heads,
-               q_heads / kc.heads, window, (float)(std::fabs((double)scale) * 1.4426950408889634),
-               scale < 0 ? 0x80008000u : 0u, -1, ws, 0, 0, 0};
+               ratio, window, (float)scale2, scale < 0 ? 0x80008000u : 0u, -1, ws, 0, 0, 0};
     for (int i = 0; i < 16; ++i)
         if (per == 1 << i) a.page_shift = i;
     return hip_status(c->dtype == PROX_BF16 ? launch_attn_bf16(a, stream) : launch_attn_f16(a, stream));

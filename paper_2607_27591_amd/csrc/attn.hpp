@@ -71,8 +71,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {   // rounded
     return __builtin_bit_cast(uint32_t, v);
 }
 // a - lo(w) and a - hi(w), what a rounding to bf16 left over (exact): one dot product each,
-// with (-1, 0) and (0, -1).  The constants stay in registers: as literals the compiler
-// encodes them wrongly.
+// with (-1, 0) and (0, -1).  The constants stay in registers: as literals of the
+// instruction their products came out as 0.
 struct Bf16Left {
     uint32_t lo = 0x0000BF80u, hi = 0xBF800000u;
     __device__ __forceinline__ Bf16Left() { asm("" : "+v"(lo), "+v"(hi)); }

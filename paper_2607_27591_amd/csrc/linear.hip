@@ -43,25 +43,26 @@ __global__ __launch_bounds__(256) void pack_linear_kernel(const uint16_t *__rest
     }
 }
 
-// Inverse view: one thread per (row, 8 inputs).
+// Inverse view: a thread takes (row, 8 inputs) items, a grid apart.
 __global__ __launch_bounds__(256) void unpack_linear_kernel(const uint8_t *__restrict__ blob, int n, int k,
                                                             int group, int8_t *__restrict__ codes,
                                                             uint16_t *__restrict__ scales) {
     const LinearLayout L(n, k, group);
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
     const int per = k / 8;
-    if (id >= (long long)n * per) return;
-    const int j = (int)(id / per), ch = (int)(id % per);
-    const int c = ch % 16;   // chunk of the block
-    const size_t blk = (size_t)(j / kLinearRows) * L.blocks + ch / 16;
-    const uint32_t word = *reinterpret_cast<const uint32_t *>(
-        blob + blk * 1024 + (size_t)((c % 4) * 16 + j % kLinearRows) * 16 + (c / 4) * 4);
+    for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < (long long)n * per;
+         id += (long long)gridDim.x * 256) {
+        const int j = (int)(id / per), ch = (int)(id % per);
+        const int c = ch % 16;   // chunk of the block
+        const size_t blk = (size_t)(j / kLinearRows) * L.blocks + ch / 16;
+        const uint32_t word = *reinterpret_cast<const uint32_t *>(
+            blob + blk * 1024 + (size_t)((c % 4) * 16 + j % kLinearRows) * 16 + (c / 4) * 4);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) codes[id * 8 + e] = (int8_t)((int)((word >> (4 * nibble_of(e))) & 15) - 8);
-    const int g = ch * 8 / group;
-    if (ch * 8 % group == 0)
-        scales[(size_t)j * L.groups + g] =
-            reinterpret_cast<const uint16_t *>(blob + L.scales)[L.scale_at(j / kLinearRows, g, j % kLinearRows)];
+        for (int e = 0; e < 8; ++e) codes[id * 8 + e] = (int8_t)((int)((word >> (4 * nibble_of(e))) & 15) - 8);
+        const int g = ch * 8 / group;
+        if (ch * 8 % group == 0)
+            scales[(size_t)j * L.groups + g] =
+                reinterpret_cast<const uint16_t *>(blob + L.scales)[L.scale_at(j / kLinearRows, g, j % kLinearRows)];
+    }
 }
 
 hipError_t launch_pack_linear(int dtype, const void *w, int n, int k, int group, void *blob, hipStream_t s) {
@@ -78,7 +79,8 @@ hipError_t launch_pack_linear(int dtype, const void *w, int n, int k, int group,
 hipError_t launch_unpack_linear(const void *blob, int n, int k, int group, int8_t *codes, uint16_t *scales,
                                 hipStream_t s) {
     const long long blocks = ((long long)n * (k / 8) + 255) / 256;
-    unpack_linear_kernel<<<(unsigned)blocks, 256, 0, s>>>(static_cast<const uint8_t *>(blob), n, k, group, codes, scales);
+    unpack_linear_kernel<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(
+        static_cast<const uint8_t *>(blob), n, k, group, codes, scales);
     return hipGetLastError();
 }
 

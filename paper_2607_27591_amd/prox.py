@@ -581,7 +581,11 @@ def _same_device(device: torch.device, *tensors) -> None:
 
 
 class _Handle:
-    """Keeps the C struct of an immutable dataclass, as a pointer to pass."""
+    """Keeps the C struct of an immutable dataclass, as a pointer to pass (which copies of
+    the object make anew)."""
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_kept"}
 
     def _pointer(self, *key):
         kept = self.__dict__.get("_kept")
@@ -708,7 +712,7 @@ def new_kv_cache(n_pages: int, page_size: int, kv_heads: int, head_dim: int, dty
 
 
 @dataclasses.dataclass(frozen=True)
-class KVSeqs:
+class KVSeqs(_Handle):
     """The sequences of a call (prox_kv_seqs): device int32 kv_len [n_seq] (the new
     tokens included), page_table [n_seq][max_pages] and, where sequences have unequal
     numbers of new tokens (at most max_new), cu_new [n_seq + 1].  max_kv bounds kv_len
@@ -846,7 +850,7 @@ def kv_attn(c: KVCache, s: KVSeqs, q: torch.Tensor, scale: Optional[float] = Non
     ws = new_kv_attn_workspace(c.head_dim, dev) if ws is None else _dev_tensor(ws, "ws", torch.uint8)
     _same_device(dev, c.blob, out, ws)
     _check(_on(dev, lib().prox_kv_attn, c.pointer(), s.pointer(dev, T), q.data_ptr(), heads, ldq,
-               c.head_dim ** -0.5 if scale is None else float(scale), int(window), out.data_ptr(), ldo,
+               c.head_dim ** -0.5 if scale is None else float(scale), min(int(window), 2 ** 31 - 1), out.data_ptr(), ldo,
                ws.data_ptr(), ws.numel()), "prox_kv_attn")
     return out
 

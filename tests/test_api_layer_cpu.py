@@ -132,6 +132,7 @@ def test_attention_refusals():
     assert _attn(heads=0) == INVALID and _attn(heads=12) == INVALID and _attn(heads=-8) == INVALID
     assert _attn(window=-1) == INVALID
     assert _attn(scale=float("nan")) == INVALID and _attn(scale=float("inf")) == INVALID
+    assert _attn(scale=3e38) == INVALID and _attn(scale=-3e38) == INVALID   # finite, but not in powers of 2
     assert _attn(q=None) == INVALID and _attn(out=None) == INVALID and _attn(ws=None) == INVALID
     assert _attn(q=FAKE + 8) == INVALID and _attn(ws=FAKE + 16) == INVALID
     assert _attn(ldq=4088) == INVALID and _attn(ldo=4100) == INVALID and _attn(ldo=8192) == INVALID

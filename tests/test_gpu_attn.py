@@ -1,4 +1,7 @@
 """Attention over the 4-bit paged cache against the 64-bit formula on what the cache holds."""
+import copy
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -181,6 +184,59 @@ def test_workspace_streams_and_graph(dtype, lens, news):
         g.replay()
         assert torch.equal(out, prox.kv_attn(case.c, case.seqs(), case.q, ws=ws))
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("news", [1, 40])
+def test_pages_past_32_bits(news):
+    # A cache of 5 GiB whose sequences stand on its first and last pages.
+    heads, dim, page = 8, 128, 128
+    per = prox.kv_bytes(heads, dim, 64, page, 1)
+    c = prox.new_kv_cache(5 * 2 ** 30 // per, page, heads, dim, BF16)
+    table = i32([[c.n_pages - 1, 0, c.n_pages - 2], [c.n_pages // 2, c.n_pages - 3, 1]])
+    lens = [300, 257]
+    k, v = (randn((sum(lens), heads, dim), i, BF16) for i in (1, 2))
+    prox.kv_append(c, prox.KVSeqs(i32(lens), table, max_new=300, cu_new=starts(lens)), k, v)
+    kw, vw = want_kv(k, v, None, c)
+    q = randn((2 * news, heads, dim), 3, BF16)
+    got = prox.kv_attn(c, prox.KVSeqs(i32(lens), table, max_new=news), q)
+    for s, a in ((0, 0), (1, 300)):
+        r = slice(s * news, (s + 1) * news)
+        ref, bound = R.attention(R.f64(q[r]), kw[a:a + lens[s]], vw[a:a + lens[s]], np.arange(lens[s] - news, lens[s]), dim ** -0.5)
+        R.check(got[r], ref, bound, BF16, f"sequence {s}")
+
+
+def test_long_prompt_of_many_heads():
+    # 9e6 rows of queries in one call.
+    n, heads, window = 70000, 128, 40
+    c = poisoned(n // 128 + 1, 128, 1, 64, BF16, group=64)
+    s = prox.KVSeqs(i32([n]), i32([range(c.n_pages)]), max_new=n)
+    k, v = (randn((n, 1, 64), i, BF16) for i in (1, 2))
+    prox.kv_append(c, s, k, v)
+    kw, vw = want_kv(k, v, None, c)
+    q = randn((500, heads, 64), 3, BF16).repeat(n // 500, 1, 1)
+    got = prox.kv_attn(c, s, q, window=window)
+    for i in (0, 1, 39, 40, 35001, n - 1):
+        a = max(i - window + 1, 0)
+        ref, bound = R.attention(R.f64(q[i:i + 1]), kw[a:i + 1], vw[a:i + 1], np.array([i - a]), 64 ** -0.5)
+        R.check(got[i:i + 1], ref, bound, BF16, f"row {i}")
+
+
+@pytest.mark.parametrize("window", [40, 2 ** 31 - 1, 2 ** 32 + 5, sys.maxsize])
+def test_window_past_the_cache(window):
+    case = Case(2, 2, 64, 32, 32, BF16, [40, 3], [2, 2])
+    assert torch.equal(prox.kv_attn(case.c, case.seqs(), case.q, window=window), prox.kv_attn(case.c, case.seqs(), case.q))
+
+
+def test_copies_of_handles():
+    case = Case(2, 2, 64, 32, 32, BF16, [40, 3], [1, 1])
+    want = prox.kv_attn(case.c, case.seqs(), case.q)
+    s = case.seqs()
+    prox.kv_attn(case.c, s, case.q)
+    c2, s2 = copy.deepcopy((case.c, s))
+    assert torch.equal(prox.kv_attn(c2, s2, case.q), want)
+    case.kv_len.zero_()                                  # the copy has lengths of its own
+    assert torch.equal(prox.kv_attn(c2, s2, case.q), want)
+    assert (prox.kv_attn(case.c, s, case.q) == 0).all()
 
 
 def test_refusals():
