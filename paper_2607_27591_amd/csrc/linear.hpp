@@ -22,10 +22,17 @@ namespace prox {
 // GPB: groups per block of 128 (4, 2, or 1 for groups of 128 and more).
 constexpr int kLinearWaves = 8;
 
-template <int NT, int RG, int WN>
+// Four waves of a block that stage a row tile each work out its offset's part for all of them
+// (28672 x 8192, 64 rows: 55.0 to 51.0 us; two waves with two tiles each: 14336 x 4096, 20.9 to
+// 21.3).
+template <int RG, int WN>
+constexpr bool kLinearShare = WN == 4 && RG / WN % 4 == 0;
+
+template <int NT, int RG, int WN, int GPB>
 constexpr size_t linear_lds() {
     constexpr int MT = (RG + 3) / 4, WK = kLinearWaves / WN, TILES = NT * MT, RT = TILES < 8 ? TILES : 8;
-    constexpr size_t stage = (WN == 1 ? 1 : 2) * (size_t)WK * MT * 4096, red = (size_t)kLinearWaves * RT * 1024;
+    constexpr size_t base = kLinearShare<RG, WN> ? GPB * 256 : 0;
+    constexpr size_t stage = (WN == 1 ? 1 : 2) * (size_t)WK * MT * (4096 + base), red = (size_t)kLinearWaves * RT * 1024;
     return stage > red ? stage : red;
 }
 
@@ -37,9 +44,15 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
     // Steps that loads run ahead: a short k is asked for at once, many rows of x take the registers.
     constexpr int DEPTH = 2;
     constexpr int XL = RG / WN;                     // loads of 4 rows of a block by each of its waves
+    // Operands of x read one product ahead (8192 x 8192, 64 rows: 22.0 to 21.0 us; 28672 x 8192
+    // 51.0 to 50.4), but with 8 loads of x in flight, whose registers it would spill (14336 x
+    // 4096, 64 rows: 21.2 to 23.5).
+    constexpr int XB = WN > 1 && XL <= 4 ? 2 : 1;
     constexpr int STAGE = WK * MT * 256;            // 16-byte chunks of x: [slot][row tile][chunk of the row][row ^ chunk]
     extern __shared__ __align__(16) unsigned char smem[];
+    constexpr bool SHARE = kLinearShare<RG, WN>;
     u32x4 *xs = reinterpret_cast<u32x4 *>(smem);
+    v4f *bs = reinterpret_cast<v4f *>(smem + 2 * (size_t)STAGE * 16);   // SHARE: [buffer][slot][row tile][group][row]
     const LinearLayout L(A.n, A.k, A.group);
     const int n = A.n, k = A.k, row0 = blockIdx.y * 4 * RG, batch = min(A.batch - row0, 4 * RG);   // rows of this workgroup
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -105,6 +118,22 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
             xs[buf * STAGE + (slot * MT + row / 16) * 256 + col * 16 + ((row % 16) ^ col)] = v[l];
         }
     };
+    // The offset's part of the row tiles that this wave has staged.
+    auto stage_base = [&](int buf) {
+#pragma unroll
+        for (int q = 0; q < XL / 4; ++q) {
+            const int m = nw * (XL / 4) + q;
+            const u32x4 *xb = xs + buf * STAGE + (slot * MT + m) * 256;
+#pragma unroll
+            for (int g = 0; g < GPB; ++g) {
+                v4f d{0, 0, 0, 0};
+#pragma unroll
+                for (int i = g * 4 / GPB; i < (g + 1) * 4 / GPB; ++i)
+                    d = mfma32<DT>(minus, __builtin_bit_cast(uint4, xb[(4 * i + h) * 16 + (col ^ (4 * i + h))]), d);
+                if (h == 0) bs[(((buf * WK + slot) * MT + m) * GPB + g) * 16 + col] = d;
+            }
+        }
+    };
     // Step j (blocks j WK + slot) computes from its LDS buffer, asks for the codes of step
     // j + DEPTH, stages the x of step j + 1 and asks for that of step j + 1 + DEPTH.
     auto step = [&](int b, int par) {
@@ -120,22 +149,34 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
         load_codes(b + DEPTH * WK, c[par], sc[par]);
         if (b < L.blocks) {
             const u32x4 *xb = xs + buf * STAGE + slot * MT * 256;
+            uint4 xf[XB][MT];
+            auto load_xf = [&](int i) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m) xf[i % XB][m] = __builtin_bit_cast(uint4, xb[m * 256 + (4 * i + h) * 16 + (col ^ (4 * i + h))]);
+            };
+#pragma unroll
+            for (int i = 0; i < XB - 1; ++i) load_xf(i);
 #pragma unroll
             for (int g = 0; g < GPB; ++g) {
                 v4f s[NT][MT], base[MT];
+                if constexpr (SHARE) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) base[m] = bs[(((buf * WK + slot) * MT + m) * GPB + g) * 16 + col];
+                }
 #pragma unroll
                 for (int i = g * 4 / GPB; i < (g + 1) * 4 / GPB; ++i) {
                     const bool first = i == g * 4 / GPB;
-                    uint4 xf[MT];
+                    if (i + XB - 1 < 4) load_xf(i + XB - 1);
+                    if constexpr (XB > 1) __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (!SHARE) {
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) xf[m] = __builtin_bit_cast(uint4, xb[m * 256 + (4 * i + h) * 16 + (col ^ (4 * i + h))]);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) base[m] = mfma32<DT>(minus, xf[m], first ? v4f{0, 0, 0, 0} : base[m]);
+                        for (int m = 0; m < MT; ++m) base[m] = mfma32<DT>(minus, xf[i % XB][m], first ? v4f{0, 0, 0, 0} : base[m]);
+                    }
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         const uint4 a = oct(cc[t][i]);
 #pragma unroll
-                        for (int m = 0; m < MT; ++m) s[t][m] = mfma32<DT>(a, xf[m], first ? v4f{0, 0, 0, 0} : s[t][m]);
+                        for (int m = 0; m < MT; ++m) s[t][m] = mfma32<DT>(a, xf[i % XB][m], first ? (SHARE ? base[m] : v4f{0, 0, 0, 0}) : s[t][m]);
                     }
                 }
 #pragma unroll
@@ -145,12 +186,16 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
 #pragma unroll
                     for (int m = 0; m < MT; ++m)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[t][m][e] = fmaf(f[e], s[t][m][e] + base[m][e], acc[t][m][e]);
+                        for (int e = 0; e < 4; ++e) acc[t][m][e] = fmaf(f[e], SHARE ? s[t][m][e] : s[t][m][e] + base[m][e], acc[t][m][e]);
                 }
             }
         }
         if constexpr (WN == 1) wave_lds_fence();   // x is this wave's own: LDS serves it in order
         if (b + WK < L.blocks) stage(buf ^ (WN == 1 ? 0 : 1), xv[next]);
+        if constexpr (SHARE) {
+            wave_lds_fence();
+            if (b + WK < L.blocks) stage_base(buf ^ 1);
+        }
         load_x(b + (DEPTH + 1) * WK, xv[next]);
         if constexpr (WN == 1) wave_lds_fence();
         else __syncthreads();
@@ -161,6 +206,10 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
         load_codes(slot + p * WK, c[p], sc[p]);
     }
     if (slot < L.blocks) stage(0, xv[0]);
+    if constexpr (SHARE) {
+        wave_lds_fence();
+        if (slot < L.blocks) stage_base(0);
+    }
     load_x(slot + DEPTH * WK, xv[0]);
     if constexpr (WN == 1) wave_lds_fence();
     else __syncthreads();
@@ -197,7 +246,7 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A)
 template <int DT, int NT, int RG, int WN, int GPB, bool TAIL>
 static hipError_t run_linear(const LinearArgs &a, hipStream_t s) {
     constexpr int R = kLinearRows * NT * WN;
-    constexpr size_t lds = linear_lds<NT, RG, WN>();
+    constexpr size_t lds = linear_lds<NT, RG, WN, GPB>();
     auto *kernel = linear_kernel<DT, NT, RG, WN, GPB, TAIL>;
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
@@ -223,12 +272,12 @@ hipError_t launch_linear_dt(const LinearArgs &a, hipStream_t s) {
     // a second one on some CUs leaves the others idle.  In us, by outputs x rows:
     //   7 rows    9973 x 3456   32: 10.3, 48: 7.6, 64: 8.5
     //   32 rows   1024 x 4096   16 x 16: 5.0, 16 x 32: 6.9      4096 x 4096  32 x 16: 7.4, 16 x 32: 8.8
-    //             8192 x 8192   32 x 32: 16.1, 64 x 32: 21.9    14336 x 4096 64 x 32: 14.2, 128 x 32: 20.8
-    //             28672 x 8192  32 x 32: 55, 64 x 32: 43, 128 x 32: 40
+    //             8192 x 8192   32 x 32: 16.1, 64 x 32: 21.9    14336 x 4096 64 x 32: 13.4, 128 x 32: 20.8
+    //             28672 x 8192  32 x 32: 55, 64 x 32: 43, 128 x 32: 39
     //   64 rows   1024 x 4096   16 x 16: 6.0, 32 x 16: 7.1, 32 x 64: 15.4
     //             4096 x 4096   64 x 16: 9.8, 32 x 32: 10.1, 32 x 64: 15.6
-    //             8192 x 8192   64 x 32: 22.1, 32 x 64: 25.8    14336 x 4096 64 x 64: 20.9, 64 x 32: 25.8
-    //             28672 x 8192  64 x 64: 78, 128 x 64: 55
+    //             8192 x 8192   64 x 32: 21.0, 32 x 64: 25.8    14336 x 4096 64 x 64: 20.9, 64 x 32: 25.8
+    //             28672 x 8192  64 x 64: 78, 128 x 64: 51
     // Up to 8 rows read little of x, and 32 outputs serve every n above (28672 x 8192, one row,
     // with 16 / 32 / 64: 26.4 / 24.6 / 27.0).
     const int cus = 256;
