@@ -33,7 +33,8 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs &A, const SeqTokens
 }
 
 // Waves per SIMD that the registers of a variant allow without spilling.
-constexpr int attn_waves(int D, int NG, int QT) {
+constexpr int attn_waves(int D, int NG, int QT, int E) {
+    if (E < 4) return D == 64 ? (NG == 1 ? 6 : 5) : D == 128 ? 4 : NG < 8 ? 3 : 2;
     if (QT == 1) return D == 64 ? 5 : D == 128 ? (NG == 4 ? 3 : 4) : (NG == 2 ? 3 : 2);
     return D == 64 ? (NG == 1 ? 3 : 2) : D == 128 ? (NG == 1 ? 3 : 2) : 1;
 }
@@ -55,10 +56,31 @@ __device__ __forceinline__ void load_words(uint32_t (&out)[W], const uint8_t *p,
     }
 }
 
-// Scale of token 4 h + e of half block j (kv_slot: 16 h + .. are this lane's 8 in a row).
-__device__ __forceinline__ float slot_scale(const u32x4 &v, int j, int e) {
-    const uint32_t w = v[2 * j + e / 2];
-    return f16_bits_to_float((e & 1) ? w >> 16 : w & 0xFFFFu);
+// Scales of a lane's E tokens of each half block (kv_slot): word e holds token e of both.
+template <int E>
+using Scales = uint32_t __attribute__((ext_vector_type(E)));
+template <int E>
+__device__ __forceinline__ Scales<E> load_scales(const uint8_t *row, int token0) {
+    return *reinterpret_cast<const Scales<E> *>(row + 4 * token0);
+}
+__device__ __forceinline__ float slot_scale(uint32_t w, int j) { return f16_bits_to_float(j ? w >> 16 : w & 0xFFFFu); }
+
+// Lanes of a row of 16 that are 4 K apart.
+template <int K>
+__device__ __forceinline__ uint32_t from_bank(uint32_t v) {   // lane i gets that of lane (i + 4 K) % 16
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + 16 - 4 * K, 0xF, 0xF, false);
+}
+template <int K>
+__device__ __forceinline__ float from_bank(float v) { return __uint_as_float(from_bank<K>(__float_as_uint(v))); }
+// Value e of the E that a lane takes of v: lanes 4 E i .. 4 E i + 4 E - 1 of a row of 16 take
+// v[E i ..].
+template <int E>
+__device__ __forceinline__ float own_of(const v4f &v, int e) {
+    int r = __float_as_int(v[e]);
+    if constexpr (E == 1) r = __builtin_amdgcn_update_dpp(r, __float_as_int(v[1]), 0xE4, 0xF, 0x2, false);
+    if constexpr (E < 4) r = __builtin_amdgcn_update_dpp(r, __float_as_int(v[2 + e]), 0xE4, 0xF, E == 1 ? 0x4 : 0xC, false);
+    if constexpr (E == 1) r = __builtin_amdgcn_update_dpp(r, __float_as_int(v[3]), 0xE4, 0xF, 0x8, false);
+    return __int_as_float(r);
 }
 
 // a * s with s an fp16 scale in place: as a fused add of 0 it is one v_fma_mix_f32, without a
@@ -98,9 +120,16 @@ __device__ __forceinline__ size_t attn_part_row(const AttnArgs &A, int split, in
 // What a wave keeps of QT tiles of 16 query rows (row l % 16 in lane l) during its pass:
 // the unnormalised output and the offset's part of it, maximum m of scale times the score,
 // the lane's part of the sum of weights l; a score above top raises m.
-template <int D, int NG, int QT>
+// E < 4: up to 4 E rows, standing 4 / E times side by side (row l % (4 E) in lane l), so that a lane
+// has E of its four tokens of a half block to weigh; the outputs of lanes 0 .. 4 E - 1 of 16 count.
+// The arithmetic of a softmax on 16 rows would bound a few rows: 16 x 8192 tokens, head_dim 128,
+// 4 rows 38.3 to 32.0 us, 8 rows 39.3 to 35.3; 131072 tokens, 4 rows 38.8 to 33.4 (group 64).
+template <int D, int NG, int QT, int E>
 struct AttnRows {
+    static_assert(E == 4 || QT == 1, "one tile");
     static constexpr int VT = D / 16, VPG = VT / NG;
+    static __device__ __forceinline__ int row_of(int lane) { return lane % (4 * E); }
+    static __device__ __forceinline__ int token0(int lane) { return lane / 16 * 4 + lane % 16 / (4 * E) * E; }
     v4f acc[QT][VT], off[QT][NG];
     float m[QT], l[QT], top[QT];
     int lo[QT], hi[QT];                    // positions that the row sees
@@ -108,10 +137,10 @@ struct AttnRows {
 
     // Rows r0 .. r1 of the sequence and kv head (the last one again past them).
     __device__ __forceinline__ void start(const AttnArgs &A, const SeqTokens &sq, int r0, int r1) {
-        const int i0 = r0 / A.ratio, i1 = r1 / A.ratio, col = lane_id() % 16;
+        const int i0 = r0 / A.ratio, i1 = r1 / A.ratio, row = row_of(lane_id());
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
-            hi[u] = sq.pos0 + min(r0 + 16 * u + col, r1) / A.ratio;
+            hi[u] = sq.pos0 + min(r0 + 16 * u + row, r1) / A.ratio;
             lo[u] = A.window > 0 ? hi[u] - A.window + 1 : 0;
             m[u] = top[u] = kAttnNone;
             l[u] = 0.0f;
@@ -129,8 +158,8 @@ struct AttnRows {
     __device__ __forceinline__ bool edge(int p0) const { return p0 + kKvBlock - 1 > hi_min || p0 < lo_max; }
 
     // Scores of the block at p0 to weights, the sums raised to a new maximum where it takes one.
-    __device__ __forceinline__ void weigh(float (&sc)[QT][2][4], int p0, bool edge, float scale, float slack) {
-        const int h = lane_id() / 16;
+    __device__ __forceinline__ void weigh(float (&sc)[QT][2][E], int p0, bool edge, float scale, float slack) {
+        const int t0 = token0(lane_id());
         uint32_t seen[QT];   // bit 4 j + e: the row sees the token
         bool up = false;
 #pragma unroll
@@ -141,8 +170,8 @@ struct AttnRows {
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int p = p0 + 16 * j + 4 * h + e;
+                    for (int e = 0; e < E; ++e) {
+                        const int p = p0 + 16 * j + t0 + e;
                         const bool ok = p <= hi[u] && p >= lo[u];
                         seen[u] |= (uint32_t)ok << (4 * j + e);
                         sc[u][j][e] = ok ? sc[u][j][e] : kAttnNone;   // whatever stands there
@@ -151,7 +180,7 @@ struct AttnRows {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[u][j][e]);
+                for (int e = 0; e < E; ++e) mx = fmaxf(mx, sc[u][j][e]);
             up |= mx > top[u];
         }
         if (__any(up)) {
@@ -161,8 +190,10 @@ struct AttnRows {
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[u][j][e]);
+                    for (int e = 0; e < E; ++e) mx = fmaxf(mx, sc[u][j][e]);
                 mx = max_swap32(max_swap16(mx));
+                if constexpr (E == 1) mx = fmaxf(mx, from_bank<1>(mx));
+                if constexpr (E < 4) mx = fmaxf(mx, from_bank<2>(mx));
                 const float m2 = fmaxf(m[u], mx * scale), f = __builtin_amdgcn_exp2f(m[u] - m2);
                 top[u] = fmaxf(top[u], mx + slack);
                 m[u] = m2;
@@ -178,7 +209,7 @@ struct AttnRows {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < E; ++e) {
                     float p = __builtin_amdgcn_exp2f(fmaf(sc[u][j][e], scale, -m[u]));
                     if (edge) p = (seen[u] >> (4 * j + e)) & 1 ? p : 0.0f;
                     sc[u][j][e] = p;
@@ -188,21 +219,21 @@ struct AttnRows {
 
     // Weights times values: value(i) is the operand of channels 16 i .. 16 i + 15, vs their scales.
     template <typename Value>
-    __device__ __forceinline__ void add(const float (&p)[QT][2][4], const u32x4 (&vs)[NG], int p0, bool edge,
+    __device__ __forceinline__ void add(const float (&p)[QT][2][E], const Scales<E> (&vs)[NG], int p0, bool edge,
                                         const Bf16Left &left, Value value) {
-        const int h = lane_id() / 16;
+        const int t0 = token0(lane_id());
         const uint4 minus = Int4Oct<kBF16>::minus();
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             uint4 ph[QT], pl[QT];
-            float f[2][4];
+            float f[2][E];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    f[j][e] = slot_scale(vs[g], j, e);
+                for (int e = 0; e < E; ++e) {
+                    f[j][e] = slot_scale(vs[g][e], j);
                     if (edge) {   // tokens that no row sees may hold anything
-                        const int q = p0 + 16 * j + 4 * h + e;
+                        const int q = p0 + 16 * j + t0 + e;
                         f[j][e] = q <= hi_max && q >= lo_min ? f[j][e] : 0.0f;
                     }
                 }
@@ -210,10 +241,24 @@ struct AttnRows {
             for (int u = 0; u < QT; ++u) {
                 uint32_t wh[4], wl[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < E; ++e) {
                     const float a = times(p[u][0][e], f[0][e]), c = times(p[u][1][e], f[1][e]);
                     wh[e] = pack_bf16(a, c);
                     wl[e] = pack_bf16(left.minus_lo(a, wh[e]), left.minus_hi(c, wh[e]));
+                }
+                if constexpr (E == 1) {   // the other lanes' tokens of the row, in the order of lanes 0 .. 4 E - 1
+                    wh[1] = from_bank<1>(wh[0]);
+                    wl[1] = from_bank<1>(wl[0]);
+                    wh[3] = from_bank<3>(wh[0]);
+                    wl[3] = from_bank<3>(wl[0]);
+                }
+                if constexpr (E < 4) {
+                    wh[2] = from_bank<2>(wh[0]);
+                    wl[2] = from_bank<2>(wl[0]);
+                }
+                if constexpr (E == 2) {
+                    wh[3] = from_bank<2>(wh[1]);
+                    wl[3] = from_bank<2>(wl[1]);
                 }
                 ph[u] = make_uint4(wh[0], wh[1], wh[2], wh[3]);
                 pl[u] = make_uint4(wl[0], wl[1], wl[2], wl[3]);
@@ -245,16 +290,16 @@ struct AttnRows {
 };
 
 // Scores of two half blocks of 16 tokens: sums of a group, base its start (the offset's part), its scales applied.
-template <int NG, int QT>
-__device__ __forceinline__ void add_scores(float (&sc)[QT][2][4], const v4f (&d)[QT][2], const u32x4 &ks, int g) {
+template <int NG, int QT, int E>
+__device__ __forceinline__ void add_scores(float (&sc)[QT][2][E], const v4f (&d)[QT][2], const Scales<E> &ks, int g) {
 #pragma unroll
     for (int u = 0; u < QT; ++u)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float f = slot_scale(ks, j, e);
-                sc[u][j][e] = g == 0 ? times(d[u][j][e], f) : fmaf(d[u][j][e], f, sc[u][j][e]);
+            for (int e = 0; e < E; ++e) {
+                const float f = slot_scale(ks[e], j), s = own_of<E>(d[u][j], e);
+                sc[u][j][e] = g == 0 ? times(s, f) : fmaf(s, f, sc[u][j][e]);
             }
 }
 
@@ -301,8 +346,8 @@ struct AttnBlocks {
 // are in flight), by VALU issue for many rows, for which QT tiles of 16 rows share the codes.
 // The four waves' results are joined through LDS, those of several workgroups of a long
 // cache by attn_join_kernel.
-template <int DT, int D, int NG, int QT>
-__global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_kernel(AttnArgs A) {
+template <int DT, int D, int NG, int QT, int E>
+__global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT, E)) void attn_kernel(AttnArgs A) {
     constexpr int R = 16 * QT, KW = D / 32, VT = D / 16, SPG = KW / NG;
     constexpr int TC = VT < 8 ? VT : 8;   // channel tiles joined at a time
     constexpr KvLayout L(D, D / NG);
@@ -328,18 +373,20 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
     const int b_end = min(sp.b0 + (split + 1) * sp.per, sp.b1);
 
     uint32_t xk[2][KW], xv[VT];
-    u32x4 xks[NG], xvs[NG];
+    using Rows = AttnRows<D, NG, QT, E>;
+    Scales<E> xks[NG], xvs[NG];
+    const int t0 = Rows::token0(lane);
     const AttnBlocks<D, NG> blocks(A, s, sp.b1);
     auto load_k = [&](const uint8_t *rec) {
         load_words(xk[0], rec, lane);
         load_words(xk[1], rec + 64 * KW * 4, lane);
 #pragma unroll
-        for (int g = 0; g < NG; ++g) xks[g] = *reinterpret_cast<const u32x4 *>(rec + L.k_scales + g * 64 + h * 16);
+        for (int g = 0; g < NG; ++g) xks[g] = load_scales<E>(rec + L.k_scales + g * 64, t0);
     };
     auto load_v = [&](const uint8_t *rec) {
         load_words(xv, rec + L.v_codes, lane);
 #pragma unroll
-        for (int g = 0; g < NG; ++g) xvs[g] = *reinterpret_cast<const u32x4 *>(rec + L.v_scales + g * 64 + h * 16);
+        for (int g = 0; g < NG; ++g) xvs[g] = load_scales<E>(rec + L.v_scales + g * 64, t0);
     };
     // Keys of the next block are asked for once this block's are used, values likewise; the
     // page of the one after it.
@@ -360,7 +407,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
 #pragma unroll
     for (int u = 0; u < QT; ++u)
         for (int w = wave; w < KW; w += kAttnWaves)
-            smem[u * KW + w][lane] = __builtin_bit_cast(v4f, query_word<D>(A, sq, head, min(r0 + 16 * u + col, r_last), w));
+            smem[u * KW + w][lane] = __builtin_bit_cast(v4f, query_word<D>(A, sq, head, min(r0 + 16 * u + Rows::row_of(lane), r_last), w));
     __syncthreads();
     for (int ug = wave; ug < QT * NG; ug += kAttnWaves) {
         v4f d{0, 0, 0, 0};
@@ -370,7 +417,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
         smem[QT * KW + ug][lane] = d;
     }
     __syncthreads();
-    AttnRows<D, NG, QT> X;
+    Rows X;
     X.start(A, sq, r0, r_last);
     const float slack = kAttnSlack / A.scale;
     int done = 0;
@@ -378,7 +425,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
         const bool ok = next_ok;
         next = blocks.record(A, head, b + kAttnWaves, b_end, next_id, next_ok);
         next_id = blocks.page_id(A, b + 2 * kAttnWaves);
-        float sc[QT][2][4];
+        float sc[QT][2][E];
         if (ok) {
             asm volatile("" ::: "memory");   // the queries stay in LDS
 #pragma unroll
@@ -398,7 +445,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
                         for (int u = 0; u < QT; ++u) d[u][j] = mfma32<DT>(a, q[u], d[u][j]);
                     }
                 }
-                add_scores<NG, QT>(sc, d, xks[g], g);
+                add_scores<NG>(sc, d, xks[g], g);
             }
         }
         load_k(next);
@@ -418,7 +465,9 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT)) void attn_k
     const size_t prow = attn_part_row(A, split, s, head, tile);
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
-        const float lw = add_swap32(add_swap16(X.l[u]));
+        float lw = add_swap32(add_swap16(X.l[u]));
+        if constexpr (E == 1) lw += from_bank<1>(lw);
+        if constexpr (E < 4) lw += from_bank<2>(lw);
         if (u > 0) __syncthreads();
         if (h == 0) {
             m_sh[wave][col] = X.m[u];
@@ -523,7 +572,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A, int R) {
     *reinterpret_cast<uint2 *>(A.out + (size_t)(sq.t0 + i) * A.ldo + (size_t)hq * D + 4 * c) = make_uint2(w0, w1);
 }
 
-template <int DT, int D, int NG, int QT>
+template <int DT, int D, int NG, int QT, int E>
 hipError_t run_attn(AttnArgs &a, hipStream_t s) {
     constexpr int R = 16 * QT;
     a.tiles = (int)(((long long)a.s.max_new * a.ratio + R - 1) / R);
@@ -537,14 +586,14 @@ hipError_t run_attn(AttnArgs &a, hipStream_t s) {
         const long long seen = ((long long)a.window + R / a.ratio + 2 * kKvBlock) / kKvBlock;
         if (seen < blocks) blocks = (int)seen;
     }
-    const long long target = 256 * attn_waves(D, NG, QT);
+    const long long target = 256 * attn_waves(D, NG, QT, E);
     long long n = blocks > kAttnWhole ? target / base : 1;
     if (n > kAttnMaxSplits) n = kAttnMaxSplits;
     a.part_rows = (int)((long long)a.s.max_new * a.ratio < R ? a.s.max_new * a.ratio : R);
     if (n > kAttnPartRows / a.part_rows / base) n = kAttnPartRows / a.part_rows / base;
     if (n > (blocks + kAttnMinBlocks - 1) / kAttnMinBlocks) n = (blocks + kAttnMinBlocks - 1) / kAttnMinBlocks;
     a.splits = n < 1 ? 1 : (int)n;
-    attn_kernel<DT, D, NG, QT><<<(unsigned)(base * a.splits), 64 * kAttnWaves, 0, s>>>(a);
+    attn_kernel<DT, D, NG, QT, E><<<(unsigned)(base * a.splits), 64 * kAttnWaves, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     const long long rows = (long long)a.s.n_seq * a.s.max_new * a.q_heads;
@@ -552,16 +601,19 @@ hipError_t run_attn(AttnArgs &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Up to 16 rows of a sequence and kv head one tile; more, two tiles a workgroup share the
+// Up to 4 and up to 8 rows of a sequence and kv head share the softmax's lanes (AttnRows). Up to
+// 16 rows one tile; more, two tiles a workgroup share the
 // codes (2 x 512 queries over 4096 tokens, group 128: 135 us against 160), but at head_dim 256,
 // where their sums leave one wave a SIMD (118 us against 180), and not four (193 us).
 template <int DT, int D, int NG>
 hipError_t launch_attn_rows(AttnArgs &a, hipStream_t s) {
     const long long rows = (long long)a.s.max_new * a.ratio;
     if constexpr (D < 256) {
-        if (rows > 16) return run_attn<DT, D, NG, 2>(a, s);
+        if (rows > 16) return run_attn<DT, D, NG, 2, 4>(a, s);
     }
-    return run_attn<DT, D, NG, 1>(a, s);
+    if (rows <= 4) return run_attn<DT, D, NG, 1, 1>(a, s);
+    if (rows <= 8) return run_attn<DT, D, NG, 1, 2>(a, s);
+    return run_attn<DT, D, NG, 1, 4>(a, s);
 }
 
 template <int DT>

@@ -279,8 +279,9 @@ __host__ __device__ constexpr int kv_k_word(int head_dim, int t, int ch) {
 }
 __host__ __device__ constexpr int kv_v_word(int lane, int i) { return ((i / 4) * 64 + lane) * 4 + i % 4; }
 
-// Place of token t of a block in a row of scales: the 8 tokens of lanes 16 h .. 16 h + 15 together.
-__host__ __device__ constexpr int kv_slot(int t) { return ((t >> 2) & 3) * 8 + (t >> 4) * 4 + (t & 3); }
+// Place of token t of a block in a row of scales: the 8 tokens of lanes 16 h .. 16 h + 15 together,
+// tokens 4 h + e and 16 + 4 h + e one word.
+__host__ __device__ constexpr int kv_slot(int t) { return ((t >> 2) & 3) * 8 + (t & 3) * 2 + (t >> 4); }
 
 struct KvLayout {
     int groups;

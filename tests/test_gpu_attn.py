@@ -71,6 +71,20 @@ SHAPES = [  # heads, ratio, dim, group, page, dtype, lengths, new tokens, window
     (1, 64, 64, 32, 64, BF16, [100, 63], [2, 1], 0),
     (2, 4, 128, 64, 64, F16, [20000], [1], 0),
     (1, 8, 128, 32, 256, BF16, [9001, 3, 5000], [2, 1, 1], 0),
+    # up to 4 and up to 8 rows of a kv head, at every head_dim and group
+    (2, 2, 256, 32, 32, BF16, [700, 40, 33], [1] * 3, 0),
+    (2, 1, 256, 64, 64, F16, [1, 95, 600], [4, 2, 3], 20),
+    (1, 4, 256, 128, 32, BF16, [45], [1], 0),
+    (1, 8, 256, 32, 64, F16, [650, 32], [1] * 2, 0),
+    (2, 3, 256, 64, 32, BF16, [77, 2], [2, 1], 31),
+    (1, 7, 256, 128, 32, F16, [300], [1], 0),
+    (3, 2, 64, 32, 32, F16, [64, 700], [2, 1], 0),
+    (2, 6, 64, 64, 96, BF16, [95, 1, 640], [1] * 3, 40),
+    (2, 3, 64, 32, 32, BF16, [0, 90], [2, 2], 1),
+    (2, 3, 128, 32, 32, BF16, [600, 31], [1] * 2, 0),
+    (4, 1, 128, 128, 64, F16, [100, 3], [3, 4], 0),
+    (2, 2, 128, 32, 32, F16, [700, 4], [3, 4], 64),
+    (1, 5, 128, 128, 32, BF16, [520, 9], [1] * 2, 0),
     # many rows of many heads: the cache is not split
     (8, 1, 128, 64, 64, BF16, [300] * 16, [70] * 16, 0),
     (16, 2, 64, 32, 32, F16, [150, 90, 400, 33, 70, 64, 100, 65], [90, 90, 130, 1, 70, 64, 3, 65], 0),
