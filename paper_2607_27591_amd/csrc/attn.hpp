@@ -576,18 +576,24 @@ template <int DT, int D, int NG, int QT, int E>
 hipError_t run_attn(AttnArgs &a, hipStream_t s) {
     constexpr int R = 16 * QT;
     a.tiles = (int)(((long long)a.s.max_new * a.ratio + R - 1) / R);
-    // Splits: as many workgroups as the chip holds at a time, one wave of each on a SIMD, no
-    // shorter than kAttnMinBlocks, as far as the partial results fit their area (twice as many,
-    // in us: 32 x 8192 tokens 41.8 instead of 40.3, 131072 tokens 41.5 instead of 37.5).  Up to
-    // kAttnWhole blocks are left whole: joining takes longer than the blocks (one launch more).
+    // Splits: at most as many workgroups as the chip holds at a time, one wave of each on a SIMD, no
+    // shorter than kAttnMinBlocks, as far as the partial results fit their area.  n workgroups of
+    // a CU pay where each has 4 n blocks (its start and its join take that long), else two or
+    // one; in us, four a CU and what is taken:
+    //   8192 tokens 11.5, 11.0;  16384 15.2, 13.2;  32768 17.8, 16.3;  8 x 2000 13.9, 12.7
+    // and with one, two, four, eight a CU:  32 x 8192, ragged 70, 45.7, 36.0, 39.5;  131072 tokens
+    // 43.7, 33.3, 33.7, 39.3.  Up to kAttnWhole blocks are left whole: joining takes longer than the
+    // blocks (one launch more).
     const long long base = (long long)a.s.n_seq * a.c.heads * a.tiles;
     int blocks = (a.s.max_kv + kKvBlock - 1) / kKvBlock;
     if (a.window > 0) {   // what the rows of a tile see at most
         const long long seen = ((long long)a.window + R / a.ratio + 2 * kKvBlock) / kKvBlock;
         if (seen < blocks) blocks = (int)seen;
     }
-    const long long target = 256 * attn_waves(D, NG, QT, E);
-    long long n = blocks > kAttnWhole ? target / base : 1;
+    const long long work = blocks * base / 256;   // blocks per CU
+    constexpr int W = attn_waves(D, NG, QT, E);
+    const int per_cu = work >= 4 * W * W ? W : work >= 15 && W > 2 ? 2 : 1;
+    long long n = blocks > kAttnWhole ? 256 * per_cu / base : 1;
     if (n > kAttnMaxSplits) n = kAttnMaxSplits;
     a.part_rows = (int)((long long)a.s.max_new * a.ratio < R ? a.s.max_new * a.ratio : R);
     if (n > kAttnPartRows / a.part_rows / base) n = kAttnPartRows / a.part_rows / base;
