@@ -70,6 +70,10 @@ template <int K>
 __device__ __forceinline__ uint32_t from_bank(uint32_t v) {   // lane i gets that of lane (i + 4 K) % 16
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + 16 - 4 * K, 0xF, 0xF, false);
 }
+template <int K, int BANKS>   // ... in the banks of a mask, old elsewhere
+__device__ __forceinline__ uint32_t take_bank(uint32_t old, uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, K == 0 ? 0xE4 : 0x120 + 16 - 4 * K, 0xF, BANKS, false);
+}
 template <int K>
 __device__ __forceinline__ float from_bank(float v) { return __uint_as_float(from_bank<K>(__float_as_uint(v))); }
 // Value e of the E that a lane takes of v: lanes 4 E i .. 4 E i + 4 E - 1 of a row of 16 take
@@ -121,9 +125,11 @@ __device__ __forceinline__ size_t attn_part_row(const AttnArgs &A, int split, in
 // the unnormalised output and the offset's part of it, maximum m of scale times the score,
 // the lane's part of the sum of weights l; a score above top raises m.
 // E < 4: up to 4 E rows, standing 4 / E times side by side (row l % (4 E) in lane l), so that a lane
-// has E of its four tokens of a half block to weigh; the outputs of lanes 0 .. 4 E - 1 of 16 count.
+// has E of its four tokens of a half block to weigh.  In the second product lanes 0 .. 4 E - 1 of
+// 16 hold the weights' first terms, the next 4 E the second (one product for both), the others
+// nothing that counts.
 // The arithmetic of a softmax on 16 rows would bound a few rows: 16 x 8192 tokens, head_dim 128,
-// 4 rows 38.3 to 32.0 us, 8 rows 39.3 to 35.3; 131072 tokens, 4 rows 38.8 to 33.4 (group 64).
+// 4 rows 38.3 to 31.1 us, 8 rows 39.3 to 34.2; 131072 tokens, 4 rows 38.8 to 32.8 (group 64).
 template <int D, int NG, int QT, int E>
 struct AttnRows {
     static_assert(E == 4 || QT == 1, "one tile");
@@ -246,24 +252,23 @@ struct AttnRows {
                     wh[e] = pack_bf16(a, c);
                     wl[e] = pack_bf16(left.minus_lo(a, wh[e]), left.minus_hi(c, wh[e]));
                 }
-                if constexpr (E == 1) {   // the other lanes' tokens of the row, in the order of lanes 0 .. 4 E - 1
-                    wh[1] = from_bank<1>(wh[0]);
-                    wl[1] = from_bank<1>(wl[0]);
-                    wh[3] = from_bank<3>(wh[0]);
-                    wl[3] = from_bank<3>(wl[0]);
-                }
-                if constexpr (E < 4) {
-                    wh[2] = from_bank<2>(wh[0]);
-                    wl[2] = from_bank<2>(wl[0]);
-                }
-                if constexpr (E == 2) {
-                    wh[3] = from_bank<2>(wh[1]);
-                    wl[3] = from_bank<2>(wl[1]);
+                if constexpr (E == 1) {   // lanes 0 .. 3 the first terms of all four tokens, 4 .. 7 the second
+                    const uint32_t a = wh[0], c = wl[0];
+                    wh[0] = take_bank<3, 0x2>(a, c);
+                    wh[1] = take_bank<0, 0x2>(from_bank<1>(a), c);
+                    wh[2] = take_bank<1, 0x2>(from_bank<2>(a), c);
+                    wh[3] = take_bank<2, 0x2>(from_bank<3>(a), c);
+                } else if constexpr (E == 2) {   // lanes 0 .. 7, 8 .. 15
+                    const uint32_t a0 = wh[0], a1 = wh[1], c0 = wl[0], c1 = wl[1];
+                    wh[0] = take_bank<2, 0xC>(a0, c0);
+                    wh[1] = take_bank<2, 0xC>(a1, c1);
+                    wh[2] = take_bank<0, 0xC>(from_bank<2>(a0), c0);
+                    wh[3] = take_bank<0, 0xC>(from_bank<2>(a1), c1);
                 }
                 ph[u] = make_uint4(wh[0], wh[1], wh[2], wh[3]);
-                pl[u] = make_uint4(wl[0], wl[1], wl[2], wl[3]);
+                if constexpr (E == 4) pl[u] = make_uint4(wl[0], wl[1], wl[2], wl[3]);
                 off[u][g] = mfma32<kBF16>(minus, ph[u], off[u][g]);
-                off[u][g] = mfma32<kBF16>(minus, pl[u], off[u][g]);
+                if constexpr (E == 4) off[u][g] = mfma32<kBF16>(minus, pl[u], off[u][g]);
             }
 #pragma unroll
             for (int i = g * VPG; i < (g + 1) * VPG; ++i) {
@@ -271,7 +276,8 @@ struct AttnRows {
 #pragma unroll
                 for (int u = 0; u < QT; ++u) acc[u][i] = mfma32<kBF16>(a, ph[u], acc[u][i]);
 #pragma unroll
-                for (int u = 0; u < QT; ++u) acc[u][i] = mfma32<kBF16>(a, pl[u], acc[u][i]);
+                for (int u = 0; u < QT; ++u)
+                    if constexpr (E == 4) acc[u][i] = mfma32<kBF16>(a, pl[u], acc[u][i]);
             }
         }
     }
@@ -494,6 +500,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT, E)) void att
                 v4f o = o_sh[i2][lane];
 #pragma unroll
                 for (int w = 1; w < kAttnWaves; ++w) o += o_sh[w * TC + i2][lane];
+                if constexpr (E < 4) {   // the two terms' products
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] += from_bank<E>(o[e]);
+                }
                 if (r >= rows) continue;
                 if (sp.eff > 1) {
                     *reinterpret_cast<v4f *>(part_o + (prow + 16 * u + col) * D + 16 * (c + i2) + 4 * h) = o;
