@@ -557,14 +557,15 @@ def add_rmsnorm(x: torch.Tensor, y: torch.Tensor, eps: float = 1e-6,
 # These calls sit between small kernels of a decode step, so they keep their own cost low:
 # a handle's C struct is built once (and again if its tensor's memory has moved), pointers go
 # as integers.
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # without the Stream object
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _on(device: torch.device, f, *args) -> int:
     """f(*args, stream) on the current stream of `device`, which may not be the
     current device."""
     index = device.index
-    if index != torch.cuda.current_device():
+    if index != _current_device():
         with torch.cuda.device(device):
             return f(*args, torch.cuda.current_stream(device).cuda_stream)
     return f(*args, torch.cuda.current_stream(device).cuda_stream if _raw_stream is None else _raw_stream(index))
@@ -587,12 +588,14 @@ class _Handle:
     def __getstate__(self):
         return {k: v for k, v in self.__dict__.items() if k != "_kept"}
 
-    def _pointer(self, *key):
-        kept = self.__dict__.get("_kept")
-        if kept is None or kept[0] != key:
-            kept = (key, ctypes.byref(self.struct()))
+    _kept = None
+
+    def _pointer(self, t: torch.Tensor):
+        kept, at, shape = self._kept, t.data_ptr(), t.shape
+        if kept is None or kept[0] != at or kept[1] != shape:
+            kept = (at, shape, ctypes.byref(self.struct()))
             object.__setattr__(self, "_kept", kept)
-        return kept[1]
+        return kept[2]
 
 
 @dataclasses.dataclass(frozen=True)
@@ -610,7 +613,7 @@ class LinearW4(_Handle):
                          self.blob.numel())
 
     def pointer(self):
-        return self._pointer(self.blob.data_ptr(), self.blob.numel())
+        return self._pointer(self.blob)
 
 
 def linear_w4_bytes(n: int, k: int, group: int = 128) -> int:
@@ -693,7 +696,7 @@ class KVCache(_Handle):
                         self.n_pages, self.blob.data_ptr(), self.blob.numel())
 
     def pointer(self):
-        return self._pointer(self.blob.data_ptr(), self.blob.numel())
+        return self._pointer(self.blob)
 
 
 def kv_bytes(kv_heads: int, head_dim: int, group: int, page_size: int, n_pages: int) -> int:
@@ -740,7 +743,7 @@ class KVSeqs(_Handle):
         """For a call of n_tokens rows on `device`."""
         key = (device, n_tokens, self.kv_len.data_ptr(), self.page_table.data_ptr(), _at(self.cu_new),
                self.kv_len.shape, self.page_table.shape)
-        kept = self.__dict__.get("_kept")
+        kept = self._kept
         if kept is None or kept[0] != key:
             _same_device(device, self.kv_len, self.page_table, self.cu_new)
             kept = (key, ctypes.byref(self.struct(n_tokens)))
@@ -762,7 +765,7 @@ class Rope(_Handle):
         return _Rope(self.table.data_ptr(), self.table.shape[0], self.table.shape[1], int(self.interleaved))
 
     def pointer(self):
-        return self._pointer(self.table.data_ptr(), self.table.shape)
+        return self._pointer(self.table)
 
 
 def _heads(t: torch.Tensor, what: str, c: KVCache, heads: int = 0):
