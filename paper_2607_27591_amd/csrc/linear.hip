@@ -7,7 +7,8 @@ namespace prox {
 
 // Packing: a workgroup takes the 16 rows of a tile over one unit of inputs (a group,
 // at least 128), 16 lanes a row, so that it writes whole blocks of 1024 bytes.  A unit of
-// 128 is read once, a longer group twice.  Bound by HBM (weights read once).
+// 128 is read once, a longer group twice.  Bound by HBM (weights read once):
+// 28672 x 8192, group 128, 246 us (590 MB, 2.4 TB/s).
 template <int DT>
 __global__ __launch_bounds__(256) void pack_linear_kernel(const uint16_t *__restrict__ w, int n, int k,
                                                           int group, uint8_t *__restrict__ blob) {

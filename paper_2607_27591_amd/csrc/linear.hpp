@@ -11,8 +11,10 @@ namespace prox {
 // y^T = W x^T as MFMAs: 16 outputs by 16 batch rows by 32 inputs each.  The codes enter as
 // exact 16-bit values with an offset, the offset's part (bias times the sum of x, one more
 // product per 32 inputs for all NT tiles) starts each group's sum, and the scale is applied
-// to the group's fp32 sum, so that nothing is rounded before y.  Bound by HBM: the codes are read
-// once.  A workgroup takes WN * NT tiles of 16 outputs over all inputs, so that no partial
+// to the group's fp32 sum, so that nothing is rounded before y.  The codes are read once: bound by
+// HBM for few rows (28672 x 8192, one row 24.6 us, 4.9 TB/s; 8192 x 8192, 16 rows 11.7 us, 3.0 TB/s
+// beside x and unpacking), by VALU, LDS and MFMA issue for many (28672 x 8192, 64 rows 51 us, 590
+// TFLOP/s, each of them a third of the time).  A workgroup takes WN * NT tiles of 16 outputs over all inputs, so that no partial
 // sums leave it; its 8 waves take NT tiles each of 8 / WN blocks of 128 inputs at a time.
 // They are added in a fixed order through LDS.
 // x goes through LDS from whole rows of 256 bytes to operand order (a load of operands
