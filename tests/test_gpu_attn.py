@@ -141,6 +141,22 @@ def test_empty_rows_are_zero_whatever_the_query_holds():
     R.check(out[:9], ref, bound, BF16, "padded")
 
 
+@pytest.mark.parametrize("ratio,news", [(4, 1), (3, 1), (4, 2), (7, 1), (16, 1), (4, 8)])
+@pytest.mark.parametrize("value", ["nan", "inf"])
+def test_a_row_spoils_no_other(ratio, news, value):
+    # One head's query of one token is NaN or infinite, over whole and split caches.
+    case = Case(2, ratio, 128, 64, 64, BF16, [40, 900], [news, news])
+    want, bound = case.want(128 ** -0.5)
+    q = case.q.clone()
+    q[news - 1, 1] = q[2 * news - 1, ratio] = float(value)
+    got = prox.kv_attn(case.c, case.seqs(), q)
+    keep = torch.ones(q.shape[:2], dtype=torch.bool)
+    keep[news - 1, 1] = keep[2 * news - 1, ratio] = False
+    R.check(got[keep.cuda()], want[keep.numpy()], bound[keep.numpy()], BF16, "other rows")
+    if value == "nan":
+        assert torch.isnan(got[~keep.cuda()]).all()
+
+
 def test_rows_past_max_new_and_bad_pages():
     case = Case(1, 2, 64, 32, 32, BF16, [200, 100], [4, 2])
     case.table[0, 2] = -5            # positions 64 .. 95 and 128 .. 159 of sequence 0 are hidden
