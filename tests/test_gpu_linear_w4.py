@@ -69,6 +69,21 @@ def test_variants(n, batch):
     _check(q, codes, scales, _randn((batch, k), 1, dtype), _randn((n,), 2, dtype), f"{n}x{k} g{group} b{batch}")
 
 
+@pytest.mark.parametrize("group,k,dtype", [(32, 1120, BF16), (32, 1280, F16), (64, 1088, F16), (64, 768, BF16), (128, 1152, F16), (384, 1536, BF16)])
+@pytest.mark.parametrize("n,batch", [(16400, 64), (16400, 37), (8200, 64), (16400, 20)])
+def test_many_rows_of_many_outputs(n, batch, group, k, dtype):
+    # Variants whose waves share the rows, over several blocks a wave, with groups inside a block and a last block in part.
+    q, codes, scales = _case(n, k, group, dtype, seed=n)
+    x = _randn((batch, k), 1, dtype)
+    _check(q, codes, scales, x, None, f"{n}x{k} g{group} b{batch}")
+    y = prox.linear_w4(q, x)
+    z = x.clone()
+    z[batch - 2] = float("nan")
+    keep = [b for b in range(batch) if b != batch - 2]
+    y2 = prox.linear_w4(q, z)
+    assert torch.equal(y[keep], y2[keep]) and torch.isnan(y2[batch - 2]).all()
+
+
 @pytest.mark.parametrize("dtype,lo,hi", [(BF16, 1e-30, 1e30), (F16, 6e-8, 6e4)])
 @pytest.mark.parametrize("batch", [1, 5, 40])
 def test_inputs_of_any_size(dtype, lo, hi, batch):
