@@ -585,6 +585,14 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A, int R) {
     *reinterpret_cast<uint2 *>(A.out + (size_t)(sq.t0 + i) * A.ldo + (size_t)hq * D + 4 * c) = make_uint2(w0, w1);
 }
 
+// Blocks that a tile of R rows sees at most.
+inline int attn_blocks(const AttnArgs &a, int R) {
+    const int all = (a.s.max_kv + kKvBlock - 1) / kKvBlock;
+    if (a.window == 0) return all;
+    const long long seen = ((long long)a.window + R / a.ratio + 2 * kKvBlock) / kKvBlock;
+    return seen < all ? (int)seen : all;
+}
+
 template <int DT, int D, int NG, int QT, int E>
 hipError_t run_attn(AttnArgs &a, hipStream_t s) {
     constexpr int R = 16 * QT;
@@ -598,11 +606,7 @@ hipError_t run_attn(AttnArgs &a, hipStream_t s) {
     // 43.7, 33.3, 33.7, 39.3.  Up to kAttnWhole blocks are left whole: joining takes longer than the
     // blocks (one launch more).
     const long long base = (long long)a.s.n_seq * a.c.heads * a.tiles;
-    int blocks = (a.s.max_kv + kKvBlock - 1) / kKvBlock;
-    if (a.window > 0) {   // what the rows of a tile see at most
-        const long long seen = ((long long)a.window + R / a.ratio + 2 * kKvBlock) / kKvBlock;
-        if (seen < blocks) blocks = (int)seen;
-    }
+    const int blocks = attn_blocks(a, R);
     const long long work = blocks * base / 256;   // blocks per CU
     constexpr int W = attn_waves(D, NG, QT, E);
     const int per_cu = work >= 4 * W * W ? W : work >= 15 && W > 2 ? 2 : 1;
@@ -623,12 +627,16 @@ hipError_t run_attn(AttnArgs &a, hipStream_t s) {
 // Up to 4 and up to 8 rows of a sequence and kv head share the softmax's lanes (AttnRows).  Up to
 // 16 rows one tile; more, two tiles a workgroup share the codes (2 x 512 queries over 4096 tokens,
 // group 128: 135 us against 160), but at head_dim 256, where their sums leave one wave a SIMD (118
-// us against 180), and not four (193 us).
+// us against 180), and not four (193 us).  One tile too where a CU has up to 32 of a tile's blocks,
+// as more workgroups are ready sooner than fewer that do less in all; in us, one and two:
+//   32 heads, 64 queries, 500 tokens 9.9, 13.8;  5 queries, 2000 10.4, 11.7;  32768 24.0, 23.3
+//   64 queries, 2000 20.1, 20.9;  8192 37.9, 35.4;  256 queries, 2000 49.3, 47.0
 template <int DT, int D, int NG>
 hipError_t launch_attn_rows(AttnArgs &a, hipStream_t s) {
     const long long rows = (long long)a.s.max_new * a.ratio;
     if constexpr (D < 256) {
-        if (rows > 16) return run_attn<DT, D, NG, 2, 4>(a, s);
+        const long long work = a.s.n_seq * ((rows + 15) / 16) * a.c.heads * attn_blocks(a, 16) / 256;   // blocks per CU
+        if (rows > 16 && work > 32) return run_attn<DT, D, NG, 2, 4>(a, s);
     }
     if (rows <= 4) return run_attn<DT, D, NG, 1, 1>(a, s);
     if (rows <= 8) return run_attn<DT, D, NG, 1, 2>(a, s);

@@ -103,6 +103,26 @@ def test_parity(heads, ratio, dim, group, page, dtype, lens, news, window):
     case.check(window, tag="tight max_kv", max_kv=max(lens) or 1)
 
 
+PAIRS = [  # as SHAPES, and pages past the longest sequence: rows and room for two tiles a workgroup
+    (2, 7, 128, 32, 256, BF16, [700, 5], [5, 5], 0, 128),
+    (2, 8, 128, 128, 256, F16, [300, 64, 33], [5, 1, 4], 0, 128),
+    (8, 4, 128, 64, 256, BF16, [900, 0, 340, 600], [300, 2, 299, 40], 150, 0),
+    (4, 7, 64, 32, 256, F16, [401, 5, 300, 333], [300, 1, 200, 133], 133, 0),
+    (4, 5, 64, 64, 256, BF16, [2, 95], [4, 4], 0, 128),
+    (1, 20, 128, 64, 256, F16, [1100] * 9, [1] * 9, 0, 128),
+    # not split
+    (8, 4, 128, 64, 64, BF16, [520] * 4, [300] * 4, 0, 0),
+    (2, 8, 128, 128, 64, F16, [700, 650, 600], [512, 300, 200], 0, 0),
+    (8, 4, 128, 32, 32, BF16, [500, 480, 470, 490], [300, 1, 299, 300], 160, 0),
+    (8, 4, 64, 64, 64, F16, [520] * 4, [300, 299, 1, 300], 0, 0),
+]
+
+
+@pytest.mark.parametrize("heads,ratio,dim,group,page,dtype,lens,news,window,slack", PAIRS)
+def test_two_tiles(heads, ratio, dim, group, page, dtype, lens, news, window, slack):
+    Case(heads, ratio, dim, group, page, dtype, lens, news, slack=slack).check(window, tag="room")
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("news", [[1, 1], [20, 20]])
 def test_peaked_and_flat_scores(dtype, news):
