@@ -167,6 +167,7 @@ prox_status prox_kv_attn(const prox_kv_cache *c, const prox_kv_seqs *s, const vo
     if (ks.n_tokens == 0) return PROX_OK;
     if (!rows_ok(q, ldq, q_heads, kc.dim) || !rows_ok(out, ldo, q_heads, kc.dim) || (q == out && ldq != ldo))
         return PROX_ERR_INVALID;
+    if (window >= ks.max_kv) window = 0;    // no row stands at max_kv or past it
     const int ratio = q_heads / kc.heads;   // at least 16 rows a workgroup (a split grid is small)
     if (ks.n_seq * (((long long)ks.max_new * ratio + 15) / 16) * kc.heads > kMaxGrid) return PROX_ERR_UNSUPPORTED;
     const int per = kc.page_size / kKvBlock;

@@ -8,29 +8,11 @@
 namespace prox {
 
 constexpr int kAttnWaves = 4;
-constexpr int kAttnMinBlocks = 4;      // blocks of 32 tokens per workgroup, before the cache is split
 constexpr int kAttnWhole = 16;         // ... that are never split
 constexpr float kAttnNone = -3.0e38f;  // running maximum before the first score (finite: no inf - inf)
 // The running maximum m of a row's scores (log2) is raised only when a score exceeds it by more
 // than this: weights stay below 2^8, and sums and outputs are rescaled a few times in all.
 constexpr float kAttnSlack = 8.0f;
-
-// Blocks that a tile of query rows sees, and how they are split: split k takes blocks
-// [b0 + k per, b0 + (k + 1) per) of [b0, b1); eff splits have any.  Row r of a sequence and kv
-// head is new token r / ratio, query head r % ratio of the kv head.
-struct AttnSpan {
-    int b0, b1, per, eff;
-};
-__device__ __forceinline__ AttnSpan attn_span(const AttnArgs &A, const SeqTokens &q, int r0, int r1) {
-    const int hi = q.pos0 + r1 / A.ratio, lo = A.window > 0 ? max(q.pos0 + r0 / A.ratio - A.window + 1, 0) : 0;
-    if (hi < 0) return AttnSpan{0, 0, 1, 0};
-    AttnSpan s;
-    s.b0 = lo / kKvBlock;
-    s.b1 = hi / kKvBlock + 1;
-    s.per = max((s.b1 - s.b0 + A.splits - 1) / A.splits, kAttnMinBlocks);
-    s.eff = (s.b1 - s.b0 + s.per - 1) / s.per;
-    return s;
-}
 
 // Waves per SIMD that the registers of a variant allow without spilling.
 constexpr int attn_waves(int D, int NG, int QT, int E) {
@@ -147,7 +129,7 @@ struct AttnRows {
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
             hi[u] = sq.pos0 + min(r0 + 16 * u + row, r1) / A.ratio;
-            lo[u] = A.window > 0 ? hi[u] - A.window + 1 : 0;
+            lo[u] = attn_first(hi[u], A.window);
             m[u] = top[u] = kAttnNone;
             l[u] = 0.0f;
 #pragma unroll
@@ -157,8 +139,8 @@ struct AttnRows {
         }
         hi_min = sq.pos0 + i0;
         hi_max = sq.pos0 + i1;
-        lo_min = A.window > 0 ? hi_min - A.window + 1 : 0;
-        lo_max = A.window > 0 ? hi_max - A.window + 1 : 0;
+        lo_min = attn_first(hi_min, A.window);
+        lo_max = attn_first(hi_max, A.window);
     }
     // Whether some row does not see all of the block at p0.
     __device__ __forceinline__ bool edge(int p0) const { return p0 + kKvBlock - 1 > hi_min || p0 < lo_max; }
@@ -376,7 +358,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_waves(D, NG, QT, E)) void att
     const SeqTokens sq = seq_tokens(A.s, s);
     const int rows = sq.n * A.ratio, r0 = tile * R;
     if (r0 >= rows) return;
-    const AttnSpan sp = attn_span(A, sq, r0, min(r0 + R, rows) - 1);
+    const AttnSpan sp = attn_span(sq, A.ratio, A.window, A.splits, r0, min(r0 + R, rows) - 1);
     if (split > 0 && split >= sp.eff) return;
     const int b_end = min(sp.b0 + (split + 1) * sp.per, sp.b1);
 
@@ -534,7 +516,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A, int R) {
     const SeqTokens sq = seq_tokens(A.s, s);
     if (i >= sq.n) return;
     const int head = hq / A.ratio, r = i * A.ratio + hq % A.ratio, tile = r / R;
-    const AttnSpan sp = attn_span(A, sq, tile * R, min((tile + 1) * R, sq.n * A.ratio) - 1);
+    const AttnSpan sp = attn_span(sq, A.ratio, A.window, A.splits, tile * R, min((tile + 1) * R, sq.n * A.ratio) - 1);
     if (sp.eff <= 1) return;
     const float *part_o = reinterpret_cast<const float *>(A.ws);
     const float2 *part_ml = reinterpret_cast<const float2 *>(part_o + (size_t)kAttnPartRows * D);

@@ -340,4 +340,28 @@ __host__ __device__ inline size_t attn_workspace_bytes(int head_dim) {
     return (size_t)kAttnPartRows * (size_t)(head_dim + 2) * 4;
 }
 
+constexpr int kAttnMinBlocks = 4;   // blocks of 32 tokens per workgroup, before the cache is split
+
+// First position that a query at position pos sees, 0 where it has no place (pos is negative there, and pos - window
+// may leave 32 bits).
+__host__ __device__ inline int attn_first(int pos, int window) { return window > 0 && pos >= window ? pos - window + 1 : 0; }
+
+// Blocks that a tile of query rows sees, and how they are split: split k takes blocks
+// [b0 + k per, b0 + (k + 1) per) of [b0, b1); eff splits have any.  Row r of a sequence and kv
+// head is new token r / ratio, query head r % ratio of the kv head.
+struct AttnSpan {
+    int b0, b1, per, eff;
+};
+__host__ __device__ inline AttnSpan attn_span(const SeqTokens &q, int ratio, int window, int splits, int r0, int r1) {
+    const int hi = q.pos0 + r1 / ratio, lo = attn_first(q.pos0 + r0 / ratio, window);
+    if (hi < 0) return AttnSpan{0, 0, 1, 0};
+    AttnSpan s;
+    s.b0 = lo / kKvBlock;
+    s.b1 = hi / kKvBlock + 1;
+    const int per = (s.b1 - s.b0 + splits - 1) / splits;
+    s.per = per > kAttnMinBlocks ? per : kAttnMinBlocks;
+    s.eff = (s.b1 - s.b0 + s.per - 1) / s.per;
+    return s;
+}
+
 }  // namespace prox

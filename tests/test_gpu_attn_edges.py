@@ -1,0 +1,22 @@
+"""Attention over the 4-bit paged cache where masks, pages and splits meet: padded sequences with windows."""
+import sys
+
+import pytest
+import torch
+
+from paper_2607_27591_amd import prox
+from test_gpu_attn import Case
+
+pytestmark = pytest.mark.gpu
+BF16, F16 = torch.bfloat16, torch.float16
+
+
+@pytest.mark.parametrize("window", [1, 2, 3, 39, 40, 41, 639, 640, 2 ** 30, 2 ** 31 - 2, 2 ** 31 - 1, 2 ** 32, sys.maxsize])
+@pytest.mark.parametrize("ratio", [1, 4, 16])
+def test_windows_of_padded_sequences(window, ratio):
+    # Sequences of fewer tokens than rows: rows without a place give 0, the others see what the window leaves.
+    case = Case(2, ratio, 64, 32, 32, BF16, [2, 40, 0, 11, 640], [5, 42, 3, 14, 7])
+    got = case.check(min(window, 10 ** 6), tag="padded")
+    assert torch.equal(prox.kv_attn(case.c, case.seqs(), case.q, window=window), got)
+    assert torch.equal(prox.kv_attn(case.c, case.seqs(max_kv=640), case.q, window=window), prox.kv_attn(case.c, case.seqs(max_kv=640), case.q, window=min(window, 640)))
+    assert (got[:3] == 0).all() and (got[5:7] == 0).all() and (got[47:50] == 0).all() and (got[50:53] == 0).all()
