@@ -571,6 +571,12 @@ def _on(device: torch.device, f, *args) -> int:
     return f(*args, torch.cuda.current_stream(device).cuda_stream if _raw_stream is None else _raw_stream(index))
 
 
+def _int32(v) -> int:
+    """v, or the nearest end of a C int: an argument past 32 bits is refused (or, a window, as good as none)
+    instead of losing its upper bits."""
+    return max(-2 ** 31, min(int(v), 2 ** 31 - 1))
+
+
 def _at(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
@@ -609,15 +615,15 @@ class LinearW4(_Handle):
 
     def struct(self) -> _W4Linear:
         _dev_tensor(self.blob, "linear blob", torch.uint8)
-        return _W4Linear(_TORCH_DT[self.dtype], self.n, self.k, self.group, self.blob.data_ptr(),
-                         self.blob.numel())
+        return _W4Linear(_TORCH_DT[self.dtype], _int32(self.n), _int32(self.k), _int32(self.group),
+                         self.blob.data_ptr(), self.blob.numel())
 
     def pointer(self):
         return self._pointer(self.blob)
 
 
 def linear_w4_bytes(n: int, k: int, group: int = 128) -> int:
-    return int(lib().prox_linear_w4_bytes(n, k, group))
+    return int(lib().prox_linear_w4_bytes(*map(_int32, (n, k, group))))
 
 
 def pack_linear_w4(w: torch.Tensor, group: int = 128) -> LinearW4:
@@ -692,15 +698,15 @@ class KVCache(_Handle):
 
     def struct(self) -> _KVCache:
         _dev_tensor(self.blob, "cache blob", torch.uint8)
-        return _KVCache(_TORCH_DT[self.dtype], self.kv_heads, self.head_dim, self.group, self.page_size,
-                        self.n_pages, self.blob.data_ptr(), self.blob.numel())
+        shape = map(_int32, (self.kv_heads, self.head_dim, self.group, self.page_size, self.n_pages))
+        return _KVCache(_TORCH_DT[self.dtype], *shape, self.blob.data_ptr(), self.blob.numel())
 
     def pointer(self):
         return self._pointer(self.blob)
 
 
 def kv_bytes(kv_heads: int, head_dim: int, group: int, page_size: int, n_pages: int) -> int:
-    return int(lib().prox_kv_bytes(kv_heads, head_dim, group, page_size, n_pages))
+    return int(lib().prox_kv_bytes(*map(_int32, (kv_heads, head_dim, group, page_size, n_pages))))
 
 
 def new_kv_cache(n_pages: int, page_size: int, kv_heads: int, head_dim: int, dtype: torch.dtype,
@@ -736,8 +742,8 @@ class KVSeqs(_Handle):
             _dev_tensor(self.cu_new, "cu_new", torch.int32)
             if self.cu_new.numel() != n + 1:
                 raise ValueError("cu_new must be [n_seq + 1]")
-        return _KVSeqs(n, self.max_new, n_tokens, self.max_kv, self.page_table.shape[1], _at(self.cu_new),
-                       self.kv_len.data_ptr(), self.page_table.data_ptr())
+        counts = map(_int32, (n, self.max_new, n_tokens, self.max_kv, self.page_table.shape[1]))
+        return _KVSeqs(*counts, _at(self.cu_new), self.kv_len.data_ptr(), self.page_table.data_ptr())
 
     def pointer(self, device: torch.device, n_tokens: int):
         """For a call of n_tokens rows on `device`."""
@@ -828,7 +834,7 @@ def kv_read(c: KVCache, s: KVSeqs, k: Optional[torch.Tensor] = None, v: Optional
 
 
 def kv_attn_workspace_bytes(head_dim: int) -> int:
-    return int(lib().prox_kv_attn_workspace_bytes(head_dim))
+    return int(lib().prox_kv_attn_workspace_bytes(_int32(head_dim)))
 
 
 def new_kv_attn_workspace(head_dim: int, device="cuda") -> torch.Tensor:
@@ -853,7 +859,7 @@ def kv_attn(c: KVCache, s: KVSeqs, q: torch.Tensor, scale: Optional[float] = Non
     ws = new_kv_attn_workspace(c.head_dim, dev) if ws is None else _dev_tensor(ws, "ws", torch.uint8)
     _same_device(dev, c.blob, out, ws)
     _check(_on(dev, lib().prox_kv_attn, c.pointer(), s.pointer(dev, T), q.data_ptr(), heads, ldq,
-               c.head_dim ** -0.5 if scale is None else float(scale), min(int(window), 2 ** 31 - 1), out.data_ptr(), ldo,
+               c.head_dim ** -0.5 if scale is None else float(scale), _int32(window), out.data_ptr(), ldo,
                ws.data_ptr(), ws.numel()), "prox_kv_attn")
     return out
 

@@ -20,3 +20,10 @@ def test_windows_of_padded_sequences(window, ratio):
     assert torch.equal(prox.kv_attn(case.c, case.seqs(), case.q, window=window), got)
     assert torch.equal(prox.kv_attn(case.c, case.seqs(max_kv=640), case.q, window=window), prox.kv_attn(case.c, case.seqs(max_kv=640), case.q, window=min(window, 640)))
     assert (got[:3] == 0).all() and (got[5:7] == 0).all() and (got[47:50] == 0).all() and (got[50:53] == 0).all()
+
+
+def test_negative_windows_are_refused():
+    case = Case(2, 2, 64, 32, 32, F16, [40], [1])
+    for window in (-1, -2 ** 31, -2 ** 32, -2 ** 32 + 7, -sys.maxsize):
+        with pytest.raises(prox.ProxError):
+            prox.kv_attn(case.c, case.seqs(), case.q, window=window)
