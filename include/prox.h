@@ -401,11 +401,14 @@ prox_status prox_add_rmsnorm(const void *x, const void *y, int batch, int d_mode
  * held in 4 bits, and attention over it.
  *
  * Projection on INT4 weights:  y_b[j] = sum_g sigma_{j,g} sum_{i in g} x_b[i]
- * q_{j,i} + bias[j], fp32 accumulation, rounded once to the dtype.  Quantised
- * as prox_w4_weights: per output j and group of `group` consecutive inputs a
+ * q_{j,i} + bias[j], rounded once to the dtype.  A block of 128 inputs (or its groups) is
+ * summed in fp32 with the codes offset by 24 and -23 in turn (fp16: 72 and -71), which
+ * comes off before the scale is applied, in fp32 too: bf16 rows need |x| of a block
+ * to sum to less than 1e37.  Quantised as prox_w4_weights: per output j and group of `group` consecutive inputs a
  * scale sigma = amax / 7 rounded to fp16, codes q = round-half-even(w / sigma)
- * clamped to [-7, 7], 0 where sigma is 0.  The blob (device, 256-byte aligned,
- * prox_linear_w4_bytes() bytes) is opaque.  All fields are inputs.
+ * clamped to [-7, 7], 0 where sigma is 0 (past amax = 7 * 65504, in bf16, sigma and every
+ * output that meets it are infinite or NaN; a NaN weight is left out of amax and
+ * gets code -7).  The blob (device, 256-byte aligned, prox_linear_w4_bytes() bytes) is opaque.  All fields are inputs.
  */
 #define PROX_MAX_LINEAR_N (1 << 20)
 #define PROX_MAX_LINEAR_K 65536
@@ -445,7 +448,9 @@ prox_status prox_linear_w4(const prox_w4_linear *q, const void *x, int64_t ldx, 
  * Key/value cache in 4 bits, in pages.  Every key and value of a kv head is
  * quantised by itself, per group of `group` consecutive channels: sigma =
  * min(amax / 7 rounded to fp16, 65504), codes c = round-half-even(x / sigma)
- * clamped to [-7, 7], 0 where sigma is 0; it stands for sigma c.  A page holds
+ * clamped to [-7, 7], 0 where sigma is 0; it stands for sigma c.  Inputs are to be
+ * finite, and the cache is in any case: an infinite one has sigma = 65504 and c = 7 or -7, a
+ * NaN is left out of amax and has c = -7 (0 where sigma is 0).  A page holds
  * page_size tokens of every kv head: head_dim + 4 head_dim / group bytes per
  * token and head, keys and values together.  The blob (device, 256-byte
  * aligned, prox_kv_bytes() bytes) is opaque and needs no initialisation.
@@ -477,7 +482,7 @@ size_t prox_kv_bytes(int kv_heads, int head_dim, int group, int page_size, int n
  *   kv_len     above max_kv counts as max_kv, below 0 as 0
  *   cu_new     entries outside [0, n_tokens] count as its nearer end, falling
  *              ones as no rows; rows past the max_new first of a sequence are
- *              left as they are
+ *              left as they are; a row that two sequences claim gets either's result
  *   page_table a position whose entry lies outside [0, n_pages) is not stored,
  *              reads as 0 and is hidden from attention
  * Two sequences may share pages that a call only reads; a page that a call
@@ -538,9 +543,15 @@ prox_status prox_kv_read(const prox_kv_cache *c, const prox_kv_seqs *s, float *k
  *   out[t][h] = sum_p softmax_p(scale q[t][h] . k[p][h']) v[p][h'],
  *   h' = h / (q_heads / kv_heads),
  * over the positions p of the token's sequence up to its own and, with window >
- * 0, only the last `window` of them (its own included).  Scores, softmax and sums
- * in fp32, out rounded once to the dtype.  Rows without a place, and rows that
- * see no position, get 0.
+ * 0, only the last `window` of them (its own included).  Scores, the softmax's maxima, weights
+ * and sum, and the sums of out are fp32, out is rounded once to the dtype.  Two
+ * things are held in less, or otherwise:
+ *   - a weight times a value's scale enters its product as two bf16 terms, which
+ *     keep it to 2^-18 of its size;
+ *   - codes enter products with an offset (24 and -23 in turn, for keys in fp16 72 and
+ *     -71) that comes off in fp32: a sum is rounded at up to that many times its terms.
+ * |q| of a group of channels (bf16) must sum to less than 1e37, and scale * score / ln 2
+ * must stay within fp32.  Rows without a place, and rows that see no position, get 0.
  *   q, out  device, token t's head h at q + t * ldq + h * head_dim (16-byte aligned;
  *           ldq, ldo multiples of 8, >= q_heads * head_dim); out may be q with ldo = ldq
  *   q_heads a multiple of kv_heads, at most 4096
