@@ -5,11 +5,12 @@ CPU only; not collected by pytest.  Run ``python tests/host_sanitizers.py``.
 1. The oracle (``oracle/oracle.c``) is built by gcc with
    ``-fsanitize=address,undefined -fno-sanitize-recover=all``. Its CPU tests
    then run in a child Python with gcc's sanitizer runtimes preloaded.
-2. ``libprox.so`` is built with the host code of ``api.hip`` (the argument
-   checks and dispatch) instrumented the same way by hipcc. The device code
-   and the other sources are built as usual. ``tests/test_api_cpu.py``, which
-   calls every entry point with invalid arguments and never reaches a HIP
-   call, then runs with clang's sanitizer runtime preloaded.
+2. ``libprox.so`` is built with the host code of ``api.hip`` and
+   ``api_layer.hip`` (the argument checks and dispatch) instrumented the same
+   way by hipcc. The device code and the other sources are built as usual.
+   ``tests/test_api_cpu.py`` and ``tests/test_api_layer_cpu.py``, which call
+   every entry point with invalid arguments and never reach a HIP call, then
+   run with clang's sanitizer runtime preloaded.
 
 Leak detection is off: the interpreter's own allocations are not ours.
 Exits non-zero on the first sanitizer report or test failure.
@@ -28,7 +29,8 @@ from paper_2607_27591_amd import build as B   # noqa: E402  (compiler flags and 
 
 ORACLE_TESTS = ["test_oracle_pins.py", "test_oracle_geglu.py", "test_oracle_threshold.py",
                 "test_oracle_w4.py", "test_cost_model.py", "test_calibrate_cpu.py"]
-API_TESTS = ["test_api_cpu.py"]
+API_SOURCES = ["api.hip", "api_layer.hip"]
+API_TESTS = ["test_api_cpu.py", "test_api_layer_cpu.py"]
 ENV = {"ASAN_OPTIONS": "detect_leaks=0:abort_on_error=0:halt_on_error=1",
        "UBSAN_OPTIONS": "halt_on_error=1:print_stacktrace=1"}
 
@@ -98,7 +100,7 @@ def api_run(tmp: str) -> int:
 
     def compile_one(src: str) -> str:
         obj = os.path.join(tmp, os.path.splitext(src)[0] + ".o")
-        extra = host_san if src == "api.hip" else []
+        extra = host_san if src in API_SOURCES else []
         r = subprocess.run([B.HIPCC, *B.CFLAGS, *extra, "-c", os.path.join(B.CSRC, src),
                             "-o", obj], capture_output=True, text=True)
         if r.returncode != 0:
@@ -111,7 +113,7 @@ def api_run(tmp: str) -> int:
     subprocess.run([B.HIPCC, "-shared", f"--offload-arch={B.ARCH}", "-fPIC", *objs, "-o", lib],
                    check=True)
     check_instrumented(lib)
-    print(f"[sanitizers] libprox built with host-instrumented api.hip: {lib}", flush=True)
+    print(f"[sanitizers] libprox built with host-instrumented {', '.join(API_SOURCES)}: {lib}", flush=True)
     return run_child("from paper_2607_27591_amd import prox\n"
                      f"prox.LIB_PATH = {lib!r}", API_TESTS, [clang_asan_runtime()])
 
