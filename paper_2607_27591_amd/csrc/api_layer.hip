@@ -127,9 +127,9 @@ prox_status prox_kv_append(const prox_kv_cache *c, const prox_kv_seqs *s, const 
     if (q && (!rows_ok(q, ldq, q_heads, kc.dim) || !rows_ok(q_out, ldq_out, q_heads, kc.dim) ||
               (q == q_out && ldq != ldq_out)))
         return PROX_ERR_INVALID;
-    const long long blocks = ((long long)ks.max_new + 2 * kKvBlock - 2) / kKvBlock;
-    if (ks.n_seq * blocks * kc.heads + (q ? (long long)ks.n_seq * ks.max_new * q_heads * (kc.dim / 8) / 256 + 1 : 0) > kMaxGrid)
-        return PROX_ERR_UNSUPPORTED;
+    const long long items = ((long long)ks.max_new + 2 * kKvBlock - 2) / kKvBlock * ks.n_seq * kc.heads;
+    if (items > kMaxGrid) return PROX_ERR_UNSUPPORTED;   // n_seq * max_new is at most 2^28 past here
+    if (q && items + (long long)ks.n_seq * ks.max_new * q_heads * (kc.dim / 8) / 256 + 1 > kMaxGrid) return PROX_ERR_UNSUPPORTED;
     return hip_status(launch_kv_append(c->dtype, kc, ks, k, ldk, v, ldv, q, q_heads, ldq, q_out, ldq_out, r, stream));
 }
 

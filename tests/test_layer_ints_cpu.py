@@ -32,3 +32,14 @@ def test_structs_keep_no_lower_bits(far, monkeypatch):
     lens, table = torch.zeros(2, dtype=torch.int32), torch.zeros((2, 3), dtype=torch.int32)
     s = prox.KVSeqs(lens, table, max_new=1 + far, max_kv=5 + far).struct(2)
     assert [s.n_seq, s.max_new, s.n_tokens, s.max_kv, s.max_pages] == [2, end, 2, end, 3]
+
+
+def test_append_grid_past_64_bits():
+    # n_seq * max_new * q_heads * head_dim / 8 = 2^63 (nothing is dereferenced or launched).
+    import ctypes
+    at = 0x100000
+    c = prox._KVCache(prox.BF16, 1, 256, 64, 32768, 1, at, 1 << 45)
+    for new in (1 << 30, (1 << 30) - 1, 1 << 29):
+        s = prox._KVSeqs(65536, new, 10, 0, 32768, at, at, at)
+        assert prox.lib().prox_kv_append(ctypes.byref(c), ctypes.byref(s), at, 256, at, 256, at, 4096, 1 << 20, at, 1 << 20,
+                                         None, None) == 2
