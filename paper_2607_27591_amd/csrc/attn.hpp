@@ -14,7 +14,8 @@ constexpr float kAttnNone = -3.0e38f;  // running maximum before the first score
 // than this: weights stay below 2^8, and sums and outputs are rescaled a few times in all.
 constexpr float kAttnSlack = 8.0f;
 
-// Waves per SIMD that the registers of a variant allow without spilling.
+// Waves per SIMD that a variant is compiled for: as many as leave none of its registers in scratch memory, or up to
+// 3 of them (head_dim 128 with 4 groups, 256 with 2 or 4, and two tiles of 128 in fp16; 8 or 16 bytes a lane).
 constexpr int attn_waves(int D, int NG, int QT, int E) {
     if (E < 4) return D == 64 ? (NG == 1 ? 6 : 5) : D == 128 ? 4 : NG < 8 ? 3 : 2;
     if (QT == 1) return D == 64 ? 5 : D == 128 ? (NG == 4 ? 3 : 4) : (NG == 2 ? 3 : 2);
@@ -331,9 +332,10 @@ struct AttnBlocks {
 // Two terms, as one bf16 term would add as much error as the rounding of a bf16 output, and
 // eight times that of an fp16 one; bf16 and not fp16, as P sv spans any range.
 // Bound by HBM for single tokens (a record is read once and contiguous; the next one's loads
-// are in flight): 131072 tokens of 8 kv heads, 32 query heads, 32.7 us with the join (143 MB, 4.4
-// TB/s).  By VALU and MFMA issue for many rows, for which QT tiles of 16 rows share the codes: 2 x
-// 512 queries over 4096 tokens, 32 heads, 135 us (470 TFLOP/s).
+// are in flight): 131072 tokens of 8 kv heads, 32 query heads, 33.4 us with the join (143 MB, 4.3
+// TB/s), the VALU busy for 70 % of this kernel's cycles.  By VALU issue for many rows, for which QT
+// tiles of 16 rows share the codes: 2 x 512 queries over 4096 tokens, 32 heads, 134 us in a stream of
+// calls (480 TFLOP/s), 153 by itself at a lower clock; VALU 75 % and MFMA 34 % of the cycles.
 // The four waves' results are joined through LDS, those of several workgroups of a long
 // cache by attn_join_kernel.
 template <int DT, int D, int NG, int QT, int E>
@@ -580,10 +582,10 @@ hipError_t run_attn(AttnArgs &a, hipStream_t s) {
     constexpr int R = 16 * QT;
     a.tiles = (int)(((long long)a.s.max_new * a.ratio + R - 1) / R);
     // Splits: at most as many workgroups as the chip holds at a time, one wave of each on a SIMD, no
-    // shorter than kAttnMinBlocks, as far as the partial results fit their area.  n workgroups of
-    // a CU pay where each has 4 n blocks (its start and its join take that long), else two or
-    // one; in us, four a CU and what is taken:
-    //   8192 tokens 11.5, 11.0;  16384 15.2, 13.2;  32768 17.8, 16.3;  8 x 2000 13.9, 12.7
+    // shorter than kAttnMinBlocks, as far as the partial results fit their area.  All W workgroups
+    // that a CU holds pay where each has 4 W blocks (its start and its join take that long), two
+    // where a CU has 15 blocks or more, else one (three is never taken, nor measured); in us, four a CU and what is taken:
+    //   8192 tokens 11.5, 11.0;  16384 15.2, 13.2;  32768 17.8, 16.3;  8 x 2000 (15 blocks) 13.9, 12.7
     // and with one, two, four, eight a CU:  32 x 8192, ragged 70, 45.7, 36.0, 39.5;  131072 tokens
     // 43.7, 33.3, 33.7, 39.3.  Up to kAttnWhole blocks are left whole: joining takes longer than the
     // blocks (one launch more).

@@ -102,9 +102,9 @@ struct AppendArgs {
     int kv_items;
 };
 
-// Bound by HBM for prompts (q, k, v and the table's rows read, q and the cache written), by a
-// chain of loads (length, page, data) for single tokens: 5.4 us for 16 of them, 26.6 us for
-// 4 x 1024 with 32 query and 8 kv heads of 128 (90 MB, 3.4 TB/s).
+// Bound for prompts by HBM (q, k, v and the table's rows read, q and the cache written) and a busy VALU
+// (59 % of the cycles), by a chain of loads (length, page, data) for single tokens: 4.8 us for 16
+// of them, 24.1 us for 4 x 1024 with 32 query and 8 kv heads of 128 (90 MB, 3.7 TB/s).
 // A workgroup takes the new tokens of one (sequence, block of 32 tokens, kv head), so that
 // each word of V codes, which holds 8 tokens of a channel, has one writer: waves 0, 1 keys,
 // waves 2, 3 values, D / 8 lanes a token.  Words that keep older tokens are read and

@@ -236,7 +236,7 @@ constexpr int kLinearRows = 16;
 constexpr int kLinearBlock = 128;
 
 // Nibble of element e (0..7) of a code word: pairs (2 p, 2 p + 1) stand 16 bits apart, so
-// that one shift and one and-or make a register of two 16-bit operands.
+// that one shift and one v_bitop3_b32 make a register of two 16-bit operands.
 __host__ __device__ constexpr int nibble_of(int e) { return (e >> 1) + 4 * (e & 1); }
 
 struct LinearLayout {

@@ -11,11 +11,11 @@ namespace prox {
 // y^T = W x^T as MFMAs: 16 outputs by 16 batch rows by 32 inputs each.  The codes enter as
 // exact 16-bit values with an offset, the offset's part (bias times the sum of x, one more
 // product per 32 inputs for all NT tiles) starts each group's sum, and the scale is applied
-// to the group's fp32 sum, so that nothing is rounded before y.  The codes are read once: bound by
-// HBM for few rows (28672 x 8192, one row 24.6 us, 4.9 TB/s; 8192 x 8192, 16 rows 11.7 us, 3.0 TB/s
-// beside x and unpacking), by VALU, LDS and MFMA issue for many (28672 x 8192, 64 rows 51 us, 590
-// TFLOP/s, each of them a third of the time).  A workgroup takes WN * NT tiles of 16 outputs over all inputs, so that no partial
-// sums leave it; its 8 waves take NT tiles each of 8 / WN blocks of 128 inputs at a time.
+// to the group's fp32 sum: nothing but fp32 sums is rounded before y.  The codes are read once: bound by
+// HBM for few rows (28672 x 8192, one row 24.6 us, 4.9 TB/s; 8192 x 8192, 16 rows 12.1 us, 2.9 TB/s
+// beside x and unpacking), by VALU, LDS and MFMA issue for many (28672 x 8192, 64 rows 51 us in a
+// stream of calls, 590 TFLOP/s, 56 by itself at a lower clock; each of them a third of the cycles).  A
+// workgroup takes WN * NT tiles of 16 outputs over all inputs, so that no partial sums leave it; its 8 waves take NT tiles each of 8 / WN blocks of 128 inputs at a time.
 // They are added in a fixed order through LDS.
 // x goes through LDS from whole rows of 256 bytes to operand order (a load of operands
 // straight from the rows touches 64 lines at a time and takes four times as long), where the
@@ -43,12 +43,12 @@ template <int DT, int NT, int RG, int WN, int GPB, bool TAIL>
 __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(LinearArgs A) {
     constexpr int MT = (RG + 3) / 4, WK = kLinearWaves / WN, TILES = NT * MT, RT = TILES < 8 ? TILES : 8;
     static_assert(RG % WN == 0, "the waves of a block load the same number of rows");
-    // Steps that loads run ahead: a short k is asked for at once, many rows of x take the registers.
+    // Steps that loads run ahead (4: 28672 x 8192, one row 24.6 to 30.4 us).
     constexpr int DEPTH = 2;
     constexpr int XL = RG / WN;                     // loads of 4 rows of a block by each of its waves
     // Operands of x read one product ahead (8192 x 8192, 64 rows: 22.0 to 21.0 us; 28672 x 8192
-    // 51.0 to 50.4), but with 8 loads of x in flight, whose registers it would spill (14336 x
-    // 4096, 64 rows: 21.2 to 23.5).
+    // 51.0 to 50.4), but with 8 loads of x in flight, which leave it no registers (14336 x 4096,
+    // 64 rows: 21.2 to 23.5).
     constexpr int XB = WN > 1 && XL <= 4 ? 2 : 1;
     constexpr int STAGE = WK * MT * 256;            // 16-byte chunks of x: [slot][row tile][chunk of the row][row ^ chunk]
     extern __shared__ __align__(16) unsigned char smem[];
@@ -281,7 +281,12 @@ hipError_t launch_linear_dt(const LinearArgs &a, hipStream_t s) {
     //             8192 x 8192   64 x 32: 21.0, 32 x 64: 25.8    14336 x 4096 64 x 64: 20.9, 64 x 32: 25.8
     //             28672 x 8192  64 x 64: 78, 128 x 64: 51
     // Up to 8 rows read little of x, and 32 outputs serve every n above (28672 x 8192, one row,
-    // with 16 / 32 / 64: 26.4 / 24.6 / 27.0).
+    // with 16 / 32 / 64: 26.4 / 24.6 / 27.0).  48 outputs are for n from 8193 to 12288 only; what
+    // n past a larger multiple of 4096 leaves idle is not taken up.
+    // The table is of groups of 128.  Groups of 64 and 32 hold two and four times the scales, and 64
+    // rows x 64 outputs keep 8 to 34 registers a lane in scratch memory then, 64 x 128 and 16 x 64 up to 5.  In us, groups
+    // 128, 64, 32, 64 rows:  14336 x 4096 20.6, 25.2, 34.1;  28672 x 8192 50.4, 55.0, 69.9;  8192 x 8192
+    // 21.0, 23.0, 27.9;  4096 x 4096 9.6, 9.8, 11.6;  16 rows, 28672 x 8192 32.2, 33.0, 38.7.
     const int cus = 256;
     auto fits = [&](int outputs, int rows) { return (n + outputs - 1) / outputs * ((batch + rows - 1) / rows) <= cus; };
     if (batch <= 4) {
