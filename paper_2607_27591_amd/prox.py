@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import operator
 import os
 from typing import List, Optional, Sequence
 
@@ -574,7 +575,7 @@ def _on(device: torch.device, f, *args) -> int:
 def _int32(v) -> int:
     """v, or the nearest end of a C int: an argument past 32 bits is refused (or, a window, as good as none)
     instead of losing its upper bits."""
-    return max(-2 ** 31, min(int(v), 2 ** 31 - 1))
+    return max(-2 ** 31, min(operator.index(v), 2 ** 31 - 1))
 
 
 def _at(t: Optional[torch.Tensor]):
@@ -859,7 +860,7 @@ def kv_attn(c: KVCache, s: KVSeqs, q: torch.Tensor, scale: Optional[float] = Non
     ws = new_kv_attn_workspace(c.head_dim, dev) if ws is None else _dev_tensor(ws, "ws", torch.uint8)
     _same_device(dev, c.blob, out, ws)
     _check(_on(dev, lib().prox_kv_attn, c.pointer(), s.pointer(dev, T), q.data_ptr(), heads, ldq,
-               c.head_dim ** -0.5 if scale is None else float(scale), _int32(window), out.data_ptr(), ldo,
+               c.head_dim ** -0.5 if scale is None else float(scale), _int32(int(window)), out.data_ptr(), ldo,
                ws.data_ptr(), ws.numel()), "prox_kv_attn")
     return out
 

@@ -34,6 +34,18 @@ def test_structs_keep_no_lower_bits(far, monkeypatch):
     assert [s.n_seq, s.max_new, s.n_tokens, s.max_kv, s.max_pages] == [2, end, 2, end, 3]
 
 
+def test_numbers_that_are_not_whole_are_refused(monkeypatch):
+    monkeypatch.setattr(prox, "_dev_tensor", lambda t, *a: t)
+    lens, table = torch.zeros(2, dtype=torch.int32), torch.zeros((2, 3), dtype=torch.int32)
+    for kw in (dict(max_new=1.5), dict(max_new=1.0), dict(max_kv=5.0), dict(max_kv="5")):
+        with pytest.raises(TypeError):
+            prox.KVSeqs(lens, table, **kw).struct(2)
+    for bad in ((8.0, 128, 64, 64, 100), (8, 128, 64, 64.5, 100)):
+        with pytest.raises(TypeError):
+            prox.kv_bytes(*bad)
+    assert prox.KVSeqs(lens, table, max_new=torch.tensor(3)).struct(2).max_new == 3
+
+
 def test_append_grid_past_64_bits():
     # n_seq * max_new * q_heads * head_dim / 8 = 2^63 (nothing is dereferenced or launched).
     import ctypes
