@@ -9,7 +9,7 @@
 namespace prox {
 
 // y^T = W x^T as MFMAs: 16 outputs by 16 batch rows by 32 inputs each.  The codes enter as
-// exact 16-bit values with an offset, the offset's part (bias times the sum of x, one more
+// exact 16-bit values with an offset, the offset's part (Int4Oct::minus times x, one more
 // product per 32 inputs for all NT tiles) starts each group's sum, and the scale is applied
 // to the group's fp32 sum: nothing but fp32 sums is rounded before y.  The codes are read once: bound by
 // HBM for few rows (28672 x 8192, one row 24.6 us, 4.9 TB/s; 8192 x 8192, 16 rows 12.1 us, 2.9 TB/s
