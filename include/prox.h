@@ -566,6 +566,86 @@ prox_status prox_kv_attn(const prox_kv_cache *c, const prox_kv_seqs *s, const vo
                          int64_t ldq, float scale, int window, void *out, int64_t ldo, void *ws,
                          size_t ws_bytes, hipStream_t stream);
 
+/*
+ * ---- Rows and weights in 8 bits (W8A8) -------------------------------------
+ *
+ * For prompts and batched decode: projections whose weights and inputs are both
+ * 8-bit integers, at any number of rows, and the two steps of a layer that make such
+ * rows, the norm before the projections and the activation before the last one.
+ *
+ * A row p of d values is held as codes c_i = round-half-even(127 p_i / A), A =
+ * max|p|, and an fp32 scale sigma that stands for A / 127; it stands for sigma c.  The
+ * codes are those of the exact quotient.  A row of zeros has sigma = 0; a row that is
+ * not finite has sigma = NaN and codes 0, so that all that is computed from it is
+ * NaN.  Codes are int8, row b at codes + b * ldc (16-byte aligned, ldc a multiple of
+ * 16, >= d; ignored for one row); scales fp32 [rows].  What reads codes may read, and
+ * ignores, the bytes behind a row's d up to a multiple of 16; they are not written.
+ * 0 <= rows <= PROX_MAX_Q8_ROWS (0: nothing is enqueued), 1 <= d <=
+ * PROX_MAX_LINEAR_K.  16-bit rows stand at any stride >= d and 2-byte alignment; 16 bytes
+ * and multiples of 8 elements are fastest.
+ */
+#define PROX_MAX_Q8_ROWS (1 << 22)
+#define PROX_MAX_Q8_PITCH (1 << 22)   /* ldc of prox_linear_w8 */
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition:
+ *   r = x + y  rounded to the dtype (y NULL: r = x),
+ *   p_i = r_i gain_i (gain NULL: 1),  n = p / sqrt(mean(r^2) + eps).
+ *   r       or NULL: where r goes
+ *   out     or NULL: n rounded to the dtype (as fp32 of 64-bit sums)
+ *   codes, scales  or both NULL: n in 8 bits; sigma = fp32(A / (127 sqrt(mean(r^2) + eps)))
+ * One of out and codes at least.  r or out may be x or y, with their stride; other
+ * overlaps are not allowed.  gain: device [d].  eps >= 0, finite; a row of zeros gives zeros for
+ * any.  One launch, no workspace.  prox_add_rmsnorm differs: its r is not rounded, and has no gain.
+ */
+prox_status prox_rmsnorm_q8(const void *x, int64_t ldx, const void *y, int64_t ldy, const void *gain, int rows,
+                            int d, prox_dtype dtype, float eps, void *r, int64_t ldr, void *out, int64_t ldo,
+                            int8_t *codes, int64_t ldc, float *scales, hipStream_t stream);
+
+/*
+ * Rows in 8 bits: of x (up NULL; act is ignored), or of p = act(x) up, rounded to
+ * fp32, as the gated FFN's last projection takes them (x, up: the gate's and up projection's
+ * rows, which may be parts of one tensor).  sigma = fp32(A / 127).
+ */
+prox_status prox_quant_q8(const void *x, int64_t ldx, const void *up, int64_t ldu, prox_act act, int rows, int d,
+                          prox_dtype dtype, int8_t *codes, int64_t ldc, float *scales, hipStream_t stream);
+
+/* What rows in 8 bits stand for, for inspection and tests: sigma c, fp32 [rows][d]. */
+prox_status prox_read_q8(const int8_t *codes, int64_t ldc, const float *scales, int rows, int d, float *out,
+                         hipStream_t stream);
+
+/*
+ * Projection on 8-bit weights:  y_b[j] = sigma_b sigma_j sum_i c_{b,i} q_{j,i} + bias[j],
+ * rounded once to the dtype.  The sum is exact (32-bit integers); its product with sigma_j
+ * and then sigma_b and the addition are fp32.  Every output's weights are a row in 8 bits as
+ * above.  The blob (device, 256-byte aligned, prox_linear_w8_bytes() bytes) is opaque.  All
+ * fields are inputs.
+ */
+typedef struct {
+    int dtype;     /* prox_dtype of bias and y (and of the weights packed from) */
+    int n;         /* outputs, 1 .. PROX_MAX_LINEAR_N */
+    int k;         /* inputs, 1 .. PROX_MAX_LINEAR_K */
+    void *blob;
+    size_t bytes;
+} prox_w8_linear;
+
+/* Bytes of the blob for this shape; 0 if unsupported. */
+size_t prox_linear_w8_bytes(int n, int k);
+
+/* Quantise w (device [n][k], q->dtype: nn.Linear's weight) into q->blob (bit-exact, deterministic). */
+prox_status prox_pack_linear_w8(const void *w, const prox_w8_linear *q, hipStream_t stream);
+
+/* Inverse view, for inspection and tests: codes int8 [n][k] and scales fp32 [n], device. */
+prox_status prox_unpack_linear_w8(const prox_w8_linear *q, int8_t *codes, float *scales, hipStream_t stream);
+
+/* The projection of rows in 8 bits (d = k; ldc <= PROX_MAX_Q8_PITCH).  codes may hold any int8.
+ *   bias  device [n] (2-byte aligned), or NULL
+ *   y     device, row b at y + b * ldy, 2-byte aligned; ldy >= n (ignored for one row)
+ * One launch, no workspace.  A row's result does not depend on the other rows, nor on
+ * their number. */
+prox_status prox_linear_w8(const prox_w8_linear *q, const int8_t *codes, int64_t ldc, const float *scales,
+                           int rows, const void *bias, void *y, int64_t ldy, hipStream_t stream);
+
 /* Static description of a status code. */
 const char *prox_strerror(prox_status status);
 

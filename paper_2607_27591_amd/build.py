@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libprox.so")
 SOURCES = ["api.hip", "api_layer.hip", "attn_bf16.hip", "attn_f16.hip", "calib.hip", "kv.hip", "linear.hip", "linear_bf16.hip",
-           "linear_f16.hip", "pack.hip", "proxy.hip", "proxy_batch.hip", "proxy_mfma.hip", "proxy_small.hip", "stage2.hip"]
+           "linear_f16.hip", "linear_w8.hip", "pack.hip", "proxy.hip", "proxy_batch.hip", "proxy_mfma.hip", "proxy_small.hip", "rows8.hip",
+           "stage2.hip"]
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -1,4 +1,4 @@
-// C-ABI of the attention half of a decoder layer (declared in include/prox.h): argument
+// C-ABI of the attention half of a decoder layer and of rows in 8 bits (declared in include/prox.h): argument
 // validation on the host, then one launch each.
 #include <prox.h>
 
@@ -6,6 +6,8 @@
 #include <cmath>
 
 #include "kernels.hpp"
+#include "linear_w8.hpp"
+#include "rows8.hpp"
 
 using namespace prox;
 
@@ -61,6 +63,30 @@ prox_status check_seqs(const prox_kv_seqs *s, const prox_kv_cache *c, KvSeqs *ou
     if (s->n_seq > 65536 || max_kv > 1 << 30 || s->max_new > 1 << 30) return PROX_ERR_UNSUPPORTED;
     *out = KvSeqs{s->cu_new, s->kv_len, s->page_table, s->n_seq, s->max_new, s->n_tokens, (int)max_kv, s->max_pages};
     return PROX_OK;
+}
+
+bool linear8_shape_ok(int n, int k) { return n >= 1 && n <= PROX_MAX_LINEAR_N && k >= 1 && k <= PROX_MAX_LINEAR_K; }
+
+prox_status check_linear8(const prox_w8_linear *q) {
+    if (!q || !q->blob || !aligned(q->blob, 256) || !dtype_ok(q->dtype)) return PROX_ERR_INVALID;
+    if (q->n < 1 || q->k < 1) return PROX_ERR_INVALID;
+    if (!linear8_shape_ok(q->n, q->k)) return PROX_ERR_UNSUPPORTED;
+    if (q->bytes < Linear8Layout(q->n, q->k).total) return PROX_ERR_WORKSPACE;
+    return PROX_OK;
+}
+
+// The shape of a call on rows in 8 bits.
+prox_status check_rows8(int rows, int d) {
+    if (rows < 0 || d < 1) return PROX_ERR_INVALID;
+    return rows > PROX_MAX_Q8_ROWS || d > PROX_MAX_LINEAR_K ? PROX_ERR_UNSUPPORTED : PROX_OK;
+}
+
+// 16-bit rows of d values with a stride of ld elements (ignored for one row).
+bool rows16_ok(const void *p, int64_t ld, int rows, int d) { return p && aligned(p, 2) && (rows == 1 || ld >= d); }
+
+// Codes: whole 16 bytes of every row can be read.
+bool codes_ok(const int8_t *codes, int64_t ld, const float *scales, int rows, int d) {
+    return codes && scales && aligned(codes, 16) && aligned(scales, 4) && (rows == 1 || (ld >= d && ld % 16 == 0));
 }
 
 // Rows of heads * dim values with a stride of ld elements.
@@ -176,6 +202,79 @@ prox_status prox_kv_attn(const prox_kv_cache *c, const prox_kv_seqs *s, const vo
     for (int i = 0; i < 16; ++i)
         if (per == 1 << i) a.page_shift = i;
     return hip_status(c->dtype == PROX_BF16 ? launch_attn_bf16(a, stream) : launch_attn_f16(a, stream));
+}
+
+prox_status prox_rmsnorm_q8(const void *x, int64_t ldx, const void *y, int64_t ldy, const void *gain, int rows, int d,
+                            prox_dtype dtype, float eps, void *r, int64_t ldr, void *out, int64_t ldo, int8_t *codes,
+                            int64_t ldc, float *scales, hipStream_t stream) {
+    if (!dtype_ok(dtype) || !(eps >= 0.0f && eps <= FLT_MAX)) return PROX_ERR_INVALID;
+    const prox_status st = check_rows8(rows, d);
+    if (st != PROX_OK) return st;
+    if (rows == 0) return PROX_OK;
+    if (!codes != !scales || (!codes && !out)) return PROX_ERR_INVALID;
+    if (!rows16_ok(x, ldx, rows, d) || (y && !rows16_ok(y, ldy, rows, d)) || !aligned(gain, 2)) return PROX_ERR_INVALID;
+    if ((r && !rows16_ok(r, ldr, rows, d)) || (out && !rows16_ok(out, ldo, rows, d)) || (r && r == out)) return PROX_ERR_INVALID;
+    if (codes && !codes_ok(codes, ldc, scales, rows, d)) return PROX_ERR_INVALID;
+    // In place only where a row keeps its place.
+    for (const void *o : {static_cast<const void *>(r), static_cast<const void *>(out)})
+        if (o && rows > 1 && ((o == x && (o == r ? ldr : ldo) != ldx) || (o == y && (o == r ? ldr : ldo) != ldy)))
+            return PROX_ERR_INVALID;
+    const NormArgs a{static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(y), static_cast<const uint16_t *>(gain),
+                     static_cast<uint16_t *>(r), static_cast<uint16_t *>(out), codes, scales, ldx, ldy, ldr, ldo, ldc, rows, d, eps};
+    return hip_status(launch_rmsnorm_q8(dtype, a, stream));
+}
+
+prox_status prox_quant_q8(const void *x, int64_t ldx, const void *up, int64_t ldu, prox_act act, int rows, int d,
+                          prox_dtype dtype, int8_t *codes, int64_t ldc, float *scales, hipStream_t stream) {
+    if (!dtype_ok(dtype) || (up && act != PROX_ACT_SILU && act != PROX_ACT_GELU)) return PROX_ERR_INVALID;
+    const prox_status st = check_rows8(rows, d);
+    if (st != PROX_OK) return st;
+    if (rows == 0) return PROX_OK;
+    if (!rows16_ok(x, ldx, rows, d) || (up && !rows16_ok(up, ldu, rows, d)) || !codes_ok(codes, ldc, scales, rows, d))
+        return PROX_ERR_INVALID;
+    const QuantArgs a{static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(up), codes, scales, ldx, ldu, ldc, rows, d, act};
+    return hip_status(launch_quant_q8(dtype, a, stream));
+}
+
+prox_status prox_read_q8(const int8_t *codes, int64_t ldc, const float *scales, int rows, int d, float *out,
+                         hipStream_t stream) {
+    const prox_status st = check_rows8(rows, d);
+    if (st != PROX_OK) return st;
+    if (rows == 0) return PROX_OK;
+    if (!codes_ok(codes, ldc, scales, rows, d) || !out || !aligned(out, 4)) return PROX_ERR_INVALID;
+    return hip_status(launch_read_q8(codes, ldc, scales, rows, d, out, stream));
+}
+
+size_t prox_linear_w8_bytes(int n, int k) { return linear8_shape_ok(n, k) ? Linear8Layout(n, k).total : 0; }
+
+prox_status prox_pack_linear_w8(const void *w, const prox_w8_linear *q, hipStream_t stream) {
+    const prox_status st = check_linear8(q);
+    if (st != PROX_OK) return st;
+    if (!w || !aligned(w, 2)) return PROX_ERR_INVALID;
+    return hip_status(launch_pack_linear_w8(q->dtype, w, q->n, q->k, q->blob, stream));
+}
+
+prox_status prox_unpack_linear_w8(const prox_w8_linear *q, int8_t *codes, float *scales, hipStream_t stream) {
+    const prox_status st = check_linear8(q);
+    if (st != PROX_OK) return st;
+    if (!codes || !scales || !aligned(scales, 4)) return PROX_ERR_INVALID;
+    return hip_status(launch_unpack_linear_w8(q->blob, q->n, q->k, codes, scales, stream));
+}
+
+prox_status prox_linear_w8(const prox_w8_linear *q, const int8_t *codes, int64_t ldc, const float *scales, int rows,
+                           const void *bias, void *y, int64_t ldy, hipStream_t stream) {
+    prox_status st = check_linear8(q);
+    if (st != PROX_OK) return st;
+    st = check_rows8(rows, q->k);
+    if (st != PROX_OK) return st;
+    if (rows == 0) return PROX_OK;
+    if (!codes_ok(codes, ldc, scales, rows, q->k) || !y || !aligned(y, 2) || !aligned(bias, 2)) return PROX_ERR_INVALID;
+    if (rows > 1 && ldy < q->n) return PROX_ERR_INVALID;
+    if (rows > 1 && ldc > PROX_MAX_Q8_PITCH) return PROX_ERR_UNSUPPORTED;   // offsets inside a tile of rows: 32 bits
+    if (((long long)rows + 15) / 16 * ((q->n + 255) / 256) > kMaxGrid) return PROX_ERR_UNSUPPORTED;
+    const Linear8Args a{static_cast<const uint8_t *>(q->blob), q->n, q->k, codes, scales, rows > 1 ? ldc : 0, rows,
+                        static_cast<const uint16_t *>(bias), static_cast<uint16_t *>(y), ldy};
+    return hip_status(launch_linear_w8(q->dtype, a, stream));
 }
 
 }  // extern "C"

@@ -257,6 +257,30 @@ struct LinearLayout {
 };
 
 // ---------------------------------------------------------------------------
+// Projections on INT8 weights and rows
+// ---------------------------------------------------------------------------
+// codes   [block of 64 outputs][block of 64 inputs, an even number][tile 0..3][lane 0..63][16]: lane l of tile t
+//         holds inputs 16 (l / 16) .. + 15 of the output w8_output(t, l % 16) of the block: its operand of a
+//         16 x 16 x 64 MFMA (or, with its pair's, of 32 x 32 x 32), and a wave's load one run of 1024 bytes.
+//         0 past n and k.
+// scales  (256-aligned) fp32 [output], 0 past n.
+// The outputs of a tile are spread so that a lane, which gets rows 4 h + e of each tile's result, has 16
+// outputs in a row from the four of them.
+constexpr int kLinear8N = 64, kLinear8K = 64;
+
+__host__ __device__ constexpr int w8_output(int tile, int row) { return 16 * (row / 4) + 4 * tile + row % 4; }
+
+struct Linear8Layout {
+    int nblocks, kblocks;
+    size_t scales, total;
+    __host__ __device__ Linear8Layout(int n, int k)
+        : nblocks((n + kLinear8N - 1) / kLinear8N), kblocks((k + 2 * kLinear8K - 1) / (2 * kLinear8K) * 2) {
+        scales = (size_t)nblocks * kblocks * (kLinear8N * kLinear8K);
+        total = align_up(scales + (size_t)nblocks * kLinear8N * 4, 256);
+    }
+};
+
+// ---------------------------------------------------------------------------
 // 4-bit paged key/value cache
 // ---------------------------------------------------------------------------
 // [page][kv head][block of 32 tokens of the page] records, each of

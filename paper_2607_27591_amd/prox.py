@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_PKG, "libprox.so")
 F16, BF16 = 0, 1
 INT8, INT4, NONE = 0, 1, 2   # NONE: unquantised 16-bit proxy (group = d_model)
 MAX_BATCH = 64   # PROX_MAX_BATCH of include/prox.h
+MAX_Q8_ROWS = MAX_Q8_PITCH = 1 << 22   # PROX_MAX_Q8_ROWS, PROX_MAX_Q8_PITCH
 SPARSE_STAGES = 3
 
 _TORCH_DT = {torch.float16: F16, torch.bfloat16: BF16}
@@ -74,6 +75,11 @@ class _KVSeqs(ctypes.Structure):
 class _Rope(ctypes.Structure):
     _fields_ = [("table", ctypes.c_void_p), ("n_pos", ctypes.c_int), ("dim", ctypes.c_int),
                 ("interleaved", ctypes.c_int)]
+
+
+class _W8Linear(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("n", ctypes.c_int), ("k", ctypes.c_int), ("blob", ctypes.c_void_p),
+                ("bytes", ctypes.c_size_t)]
 
 
 _lib = None
@@ -139,6 +145,15 @@ def lib() -> ctypes.CDLL:
         L.prox_kv_attn_workspace_bytes.argtypes = [I]
         L.prox_kv_attn_workspace_bytes.restype = S
         L.prox_kv_attn.argtypes = [CP, KP, P, I, N, Z, I, P, N, P, S, P]
+        L8 = ctypes.POINTER(_W8Linear)
+        L.prox_rmsnorm_q8.argtypes = [P, N, P, N, P, I, I, I, Z, P, N, P, N, P, N, P, P]
+        L.prox_quant_q8.argtypes = [P, N, P, N, I, I, I, I, P, N, P, P]
+        L.prox_read_q8.argtypes = [P, N, P, I, I, P, P]
+        L.prox_linear_w8_bytes.argtypes = [I, I]
+        L.prox_linear_w8_bytes.restype = S
+        L.prox_pack_linear_w8.argtypes = [P, L8, P]
+        L.prox_unpack_linear_w8.argtypes = [L8, P, P, P]
+        L.prox_linear_w8.argtypes = [L8, P, N, P, I, P, P, N, P]
         L.prox_strerror.argtypes = [I]
         L.prox_strerror.restype = ctypes.c_char_p
         for name in ("prox_pack_proxy", "prox_unpack_proxy", "prox_ffn_dense", "prox_ffn_sparse",
@@ -146,7 +161,9 @@ def lib() -> ctypes.CDLL:
                      "prox_reservoir_add", "prox_quantile_threshold", "prox_allocate_sparsity",
                      "prox_pack_w4", "prox_unpack_w4", "prox_ffn_dense_w4", "prox_ffn_sparse_w4",
                      "prox_ffn_sparse_tau_w4", "prox_pack_linear_w4", "prox_unpack_linear_w4",
-                     "prox_linear_w4", "prox_kv_append", "prox_kv_read", "prox_kv_attn"):
+                     "prox_linear_w4", "prox_kv_append", "prox_kv_read", "prox_kv_attn",
+                     "prox_rmsnorm_q8", "prox_quant_q8", "prox_read_q8", "prox_pack_linear_w8",
+                     "prox_unpack_linear_w8", "prox_linear_w8"):
             getattr(L, name).restype = I
         _lib = L
     return _lib
@@ -863,6 +880,188 @@ def kv_attn(c: KVCache, s: KVSeqs, q: torch.Tensor, scale: Optional[float] = Non
                c.head_dim ** -0.5 if scale is None else float(scale), _int32(int(window)), out.data_ptr(), ldo,
                ws.data_ptr(), ws.numel()), "prox_kv_attn")
     return out
+
+
+# ---------------------------------------------------------------------------
+# Rows and weights in 8 bits
+# ---------------------------------------------------------------------------
+
+@dataclasses.dataclass(frozen=True)
+class RowsQ8:
+    """Rows in 8 bits: device codes int8 [rows][d], whose rows stand a multiple of 16 bytes apart, and scales
+    float32 [rows]; row b stands for scales[b] * codes[b].  Some of the rows: RowsQ8(q.codes[a:b], q.scales[a:b])."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    def check(self):
+        """(rows, d, row stride)."""
+        c, s = self.codes, self.scales
+        if c.dim() != 2:
+            raise ValueError("codes must be [rows][d]")
+        rows, ld = _rows2(c, "codes", torch.int8, c.shape[1])
+        _dev_tensor(s, "scales", torch.float32)
+        if tuple(s.shape) != (rows,):
+            raise ValueError("scales must be [rows]")
+        return rows, c.shape[1], ld
+
+
+def new_rows_q8(rows: int, d: int, device="cuda") -> RowsQ8:
+    rows, d = operator.index(rows), operator.index(d)
+    return RowsQ8(torch.empty((rows, (d + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :d],
+                  torch.empty(rows, dtype=torch.float32, device=device))
+
+
+def _rows16(x: torch.Tensor, what: str):
+    """(rows, d, row stride) of 16-bit rows [rows][d], or [d]."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in _TORCH_DT:
+        raise ValueError(f"{what} must be float16 or bfloat16")
+    if not 1 <= x.dim() <= 2:
+        raise ValueError(f"{what} must be [rows][d]")
+    rows, ld = _rows2(x, what, x.dtype, x.shape[-1])
+    return rows, x.shape[-1], ld
+
+
+def _like(t: Optional[torch.Tensor], what: str, x: torch.Tensor, rows: int, d: int) -> int:
+    """Row stride of t, which has x's rows (0 without t)."""
+    if t is None:
+        return 0
+    n, ld = _rows2(t, what, x.dtype, d)
+    if n != rows:
+        raise ValueError(f"{what} must have the rows of x")
+    return ld
+
+
+def _q8_out(q: Optional[RowsQ8], rows: int, d: int, device):
+    """(q, row stride): rows to write to, made when not given."""
+    q = new_rows_q8(rows, d, device) if q is None else q
+    n, w, ld = q.check()
+    if (n, w) != (rows, d):
+        raise ValueError("q must have the shape of x")
+    return q, ld
+
+
+def _norm(x, y, gain, eps, residual, out, q):
+    rows, d, ldx = _rows16(x, "x")
+    ldy, ldr, ldo = (_like(t, n, x, rows, d) for t, n in ((y, "y"), (residual, "residual"), (out, "out")))
+    ldc = 0
+    if q is not None:
+        q, ldc = _q8_out(q, rows, d, x.device)
+    if gain is not None:
+        _dev_tensor(gain, "gain", x.dtype)
+        if gain.numel() != d:
+            raise ValueError("gain must be [d]")
+    codes, scales = (None, None) if q is None else (q.codes, q.scales)
+    _same_device(x.device, y, gain, residual, out, codes, scales)
+    _check(_on(x.device, lib().prox_rmsnorm_q8, x.data_ptr(), ldx, _at(y), ldy, _at(gain), rows, d, _TORCH_DT[x.dtype],
+               float(eps), _at(residual), ldr, _at(out), ldo, _at(codes), ldc, _at(scales)), "prox_rmsnorm_q8")
+
+
+def rmsnorm(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
+            residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Root-mean-square norm of the rows r = x + y (x without y), times gain [d], in their own type.  r, rounded to
+    that type, goes to `residual` where given; residual or out may be x or y."""
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    _norm(x, y, gain, eps, residual, out, None)
+    return out
+
+
+def rmsnorm_q8(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
+               residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+               q: Optional[RowsQ8] = None) -> RowsQ8:
+    """rmsnorm with its result in 8 bits (q, made when not given), and in the rows' own type too where `out` is given."""
+    if q is None:
+        rows, d, _ = _rows16(x, "x")
+        q = new_rows_q8(rows, d, x.device)
+    _norm(x, y, gain, eps, residual, out, q)
+    return q
+
+
+def quant_q8(x: torch.Tensor, up: Optional[torch.Tensor] = None, act: int = SILU, q: Optional[RowsQ8] = None) -> RowsQ8:
+    """Rows in 8 bits: of x, or of act(x) * up (SILU or GELU)."""
+    rows, d, ldx = _rows16(x, "x")
+    ldu = _like(up, "up", x, rows, d)
+    q, ldc = _q8_out(q, rows, d, x.device)
+    _same_device(x.device, up, q.codes, q.scales)
+    _check(_on(x.device, lib().prox_quant_q8, x.data_ptr(), ldx, _at(up), ldu, _int32(act), rows, d, _TORCH_DT[x.dtype],
+               q.codes.data_ptr(), ldc, q.scales.data_ptr()), "prox_quant_q8")
+    return q
+
+
+def read_q8(q: RowsQ8, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """What rows in 8 bits stand for: float32 [rows][d]."""
+    rows, d, ldc = q.check()
+    out = torch.empty((rows, d), dtype=torch.float32, device=q.codes.device) if out is None else _dev_tensor(out, "out", torch.float32)
+    if tuple(out.shape) != (rows, d):
+        raise ValueError("out must be [rows][d]")
+    _same_device(q.codes.device, q.scales, out)
+    _check(_on(out.device, lib().prox_read_q8, q.codes.data_ptr(), ldc, q.scales.data_ptr(), rows, d, out.data_ptr()), "prox_read_q8")
+    return out
+
+
+@dataclasses.dataclass(frozen=True)
+class LinearW8(_Handle):
+    """A projection's weights in INT8 with a scale an output (W8A8): an opaque device blob."""
+    blob: torch.Tensor
+    dtype: torch.dtype
+    n: int
+    k: int
+
+    def struct(self) -> _W8Linear:
+        _dev_tensor(self.blob, "linear blob", torch.uint8)
+        return _W8Linear(_TORCH_DT[self.dtype], _int32(self.n), _int32(self.k), self.blob.data_ptr(), self.blob.numel())
+
+    def pointer(self):
+        return self._pointer(self.blob)
+
+
+def linear_w8_bytes(n: int, k: int) -> int:
+    return int(lib().prox_linear_w8_bytes(_int32(n), _int32(k)))
+
+
+def pack_linear_w8(w: torch.Tensor) -> LinearW8:
+    """Quantise nn.Linear's weight w [n][k] (float16 or bfloat16), a scale an output."""
+    if w.dtype not in _TORCH_DT:
+        raise ValueError("weights must be float16 or bfloat16")
+    _dev_tensor(w, "w")
+    if w.dim() != 2:
+        raise ValueError("w must be [n][k]")
+    n, k = w.shape
+    size = linear_w8_bytes(n, k)
+    if size == 0:
+        raise ProxError(2, "prox_linear_w8_bytes")
+    q = LinearW8(torch.empty(size, dtype=torch.uint8, device=w.device), w.dtype, n, k)
+    _check(_on(w.device, lib().prox_pack_linear_w8, _at(w), q.pointer()), "prox_pack_linear_w8")
+    return q
+
+
+def unpack_linear_w8(q: LinearW8):
+    """(codes int8 [n][k], scales float32 [n])."""
+    dev = q.blob.device
+    codes = torch.empty((q.n, q.k), dtype=torch.int8, device=dev)
+    scales = torch.empty(q.n, dtype=torch.float32, device=dev)
+    _check(_on(dev, lib().prox_unpack_linear_w8, q.pointer(), _at(codes), _at(scales)), "prox_unpack_linear_w8")
+    return codes, scales
+
+
+def linear_w8(w: LinearW8, x: RowsQ8, bias: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rows in 8 bits times the INT8 weights, plus bias [n]: [rows][n] in the weights' type; rows of y may stand apart."""
+    rows, k, ldc = x.check()
+    if k != w.k:
+        raise ValueError(f"x must be [rows][{w.k}]")
+    dev = x.codes.device
+    if y is None:
+        y = torch.empty((rows, w.n), dtype=w.dtype, device=dev)
+    n, ldy = _rows2(y, "y", w.dtype, w.n)
+    if n != rows:
+        raise ValueError("y must have the rows of x")
+    if bias is not None:
+        _dev_tensor(bias, "bias", w.dtype)
+        if bias.numel() != w.n:
+            raise ValueError("bias must be [n]")
+    _same_device(dev, w.blob, x.scales, y, bias)
+    _check(_on(dev, lib().prox_linear_w8, w.pointer(), x.codes.data_ptr(), ldc, x.scales.data_ptr(), rows, _at(bias),
+               y.data_ptr(), ldy), "prox_linear_w8")
+    return y
 
 
 def from_bits(bits, dtype_code: int, device="cuda") -> torch.Tensor:

@@ -1,0 +1,330 @@
+"""Rows in 8 bits: the norm and the activation that make them, against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import rows8_ref as R
+from layer_ref import f64
+from paper_2607_27591_amd import prox
+
+pytestmark = pytest.mark.gpu
+BF16, F16 = torch.bfloat16, torch.float16
+
+
+def randn(shape, seed, dtype, scale=1.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * scale).to(dtype).cuda()
+
+
+def hidden(rows, d, seed, dtype):
+    x = torch.randn((rows, d), generator=torch.Generator().manual_seed(seed))
+    x[:, ::97] *= 20
+    return x.to(dtype).cuda()
+
+
+def strided(x, pad, lead=0):
+    """The same rows inside wider ones."""
+    wide = torch.full((x.shape[0], x.shape[1] + pad + lead), 9.0, dtype=x.dtype, device="cuda")
+    wide[:, lead:lead + x.shape[1]] = x
+    return wide[:, lead:lead + x.shape[1]]
+
+
+def guarded_q8(rows, d, more=16):
+    """Rows to write to, with marks behind each."""
+    pitch = (d + 15) // 16 * 16 + more
+    codes = torch.full((rows, pitch), 77, dtype=torch.int8, device="cuda")
+    return prox.RowsQ8(codes[:, :d], torch.full((rows,), 5.0, device="cuda")), codes
+
+
+def check_norm(x, y, gain, eps, tag, what="both"):
+    rows, d = x.shape
+    q, whole = guarded_q8(rows, d)
+    res, out = torch.full_like(x, 3.0), torch.full_like(x, 3.0)
+    got = prox.rmsnorm_q8(x, y, gain, eps, residual=res, out=out, q=q)
+    assert got is q and (whole[:, d:] == 77).all(), tag
+    r, n, c, s = R.norm(f64(x), None if y is None else f64(y), None if gain is None else f64(gain), eps, x.dtype)
+    assert np.array_equal(f64(res), r, equal_nan=True), f"{tag}: residual"
+    R.check_codes(q.codes, c, tag)
+    R.check_scales(q.scales, s, tag)
+    R.check_out(out, n, x.dtype, tag)
+    # Each output by itself is the same.
+    assert torch.equal(prox.rmsnorm(x, y, gain, eps).view(torch.int16), out.view(torch.int16))
+    alone = prox.rmsnorm_q8(x, y, gain, eps)
+    assert torch.equal(alone.codes, q.codes) and torch.equal(alone.scales.view(torch.int32), q.scales.view(torch.int32))
+    return q
+
+
+WIDTHS = [1, 2, 7, 8, 9, 63, 64, 65, 127, 504, 511, 512, 513, 520, 1024, 1031, 2047, 2048, 2049, 4096, 5000, 8191, 8192, 8193,
+          12288, 16384, 16391, 32768, 32776, 65535, 65536]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_norm_widths(d, dtype):
+    rows = 5
+    check_norm(hidden(rows, d, d, dtype), randn((rows, d), d + 1, dtype), (1 + randn((d,), 3, torch.float32, 0.3)).to(dtype), 1e-6, f"{d}")
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 17, 255, 256, 257, 300, 1025])
+@pytest.mark.parametrize("d", [200, 1111, 4096])
+def test_norm_rows(rows, d):
+    check_norm(hidden(rows, d, rows, BF16), hidden(rows, d, rows + 1, BF16), randn((d,), 3, BF16), 1e-5, f"{rows}x{d}")
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("gain", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_norm_without(add, gain, dtype):
+    check_norm(hidden(7, 1000, 1, dtype), randn((7, 1000), 2, dtype) if add else None, randn((1000,), 3, dtype) if gain else None, 0.0, "")
+
+
+@pytest.mark.parametrize("lead", [0, 1, 3, 8])
+@pytest.mark.parametrize("d,pad", [(1000, 0), (999, 2), (1024, 1), (2056, 8)])
+def test_norm_strides_and_alignments(d, pad, lead):
+    x, y, gain = hidden(6, d, 1, BF16), randn((6, d), 2, BF16), randn((d + 1,), 3, BF16)[lead % 2:][:d].clone()
+    want = prox.rmsnorm_q8(x, y, gain)
+    wout = prox.rmsnorm(x, y, gain)
+    res, out = strided(x, pad + 3, lead), strided(x, pad, lead + 1)
+    base = torch.full((d + 9,), 1.0, dtype=BF16, device="cuda")
+    base[lead:lead + d] = gain
+    got = prox.rmsnorm_q8(strided(x, pad, lead), strided(y, pad + 1, lead), base[lead:lead + d], residual=res, out=out)
+    assert torch.equal(got.codes, want.codes) and torch.equal(got.scales, want.scales) and torch.equal(out, wout)
+    assert torch.equal(res, (x.float() + y.float()).to(BF16))
+    for t, n in ((res, pad + 3 + lead), (out, pad + lead + 1)):      # nothing beside the rows is written
+        whole = t._base if t._base is not None else t
+        assert (whole.float() == 9).sum() >= 6 * n - 0 and whole.shape[1] == d + n
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("d", [520, 4100])
+def test_norm_in_place(d, dtype):
+    x, y, gain = hidden(9, d, 1, dtype), randn((9, d), 2, dtype), randn((d,), 3, dtype)
+    r, n = torch.empty_like(x), torch.empty_like(x)
+    want = prox.rmsnorm_q8(x, y, gain, residual=r, out=n)
+    a, b = x.clone(), y.clone()
+    got = prox.rmsnorm_q8(a, b, gain, residual=a, out=b)
+    assert torch.equal(a, r) and torch.equal(b, n) and torch.equal(got.codes, want.codes) and torch.equal(got.scales, want.scales)
+    a, b = x.clone(), y.clone()
+    prox.rmsnorm(a, b, gain, residual=b, out=a)
+    assert torch.equal(b, r) and torch.equal(a, n)
+
+
+def test_norm_of_one_vector():
+    x, y = hidden(1, 777, 1, BF16)[0], randn((777,), 2, BF16)
+    out = prox.rmsnorm(x, y)
+    assert out.shape == (777,) and torch.equal(out[None], prox.rmsnorm(x[None], y[None]))
+    assert prox.rmsnorm_q8(x).codes.shape == (1, 777)
+
+
+EXTREMES = {
+    "zeros": lambda d: np.zeros(d),
+    "one of them": lambda d: np.eye(1, d, d // 2)[0] * 3,
+    "alike": lambda d: np.full(d, -2.5),
+    "tiny": lambda d: np.linspace(-1, 1, d) * 1e-39,
+    "smallest": lambda d: np.where(np.arange(d) % 3, 0, 2.0 ** -133),
+    "huge": lambda d: np.linspace(-1, 1, d) * 3e38,
+    "wide": lambda d: 2.0 ** np.linspace(-120, 120, d),
+    "ties": lambda d: (np.arange(d) % 255 - 127) / 2.0 * (1 - 2 * (np.arange(d) % 2)),
+    "halves": lambda d: np.where(np.arange(d) == 5, 127.0, np.arange(d) % 127 + 0.5),
+}
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+@pytest.mark.parametrize("d", [96, 1500, 9000])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_norm_extremes(d, dtype, eps):
+    limit = 6e4 if dtype == F16 else 3.3e38
+    x = torch.from_numpy(np.stack([np.clip(f(d), -limit, limit) for f in EXTREMES.values()])).to(dtype).cuda()
+    check_norm(x, None, None, eps, "unit gain")
+    check_norm(x, None, randn((d,), 5, dtype), eps, "gain")
+    check_norm(x, None, torch.zeros(d, dtype=dtype, device="cuda"), eps, "gain 0")
+    if dtype == BF16:
+        for g in (1e-37, 1e30):
+            check_norm(x, None, torch.full((d,), g, dtype=dtype, device="cuda"), eps, f"gain {g}")
+
+
+@pytest.mark.parametrize("d", [96, 1500, 9000])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_norm_not_finite(d, dtype):
+    x, y, gain = hidden(8, d, 1, dtype), randn((8, d), 2, dtype), randn((d,), 3, dtype)
+    x[1, 5], y[2, d - 1], x[3, 0], x[4, 7], y[4, 7] = float("nan"), float("nan"), float("inf"), float("inf"), -float("inf")
+    big = torch.finfo(dtype).max
+    x[5, 3], y[5, 3] = big, big           # the residual overflows
+    check_norm(x, y, gain, 1e-6, "rows")
+    q = check_norm(x, y, None, 1e-6, "no gain")
+    assert torch.isnan(q.scales).tolist() == [False, True, True, True, True, True, False, False]
+    gain[2] = float("inf")
+    check_norm(x, y, gain, 1e-6, "gain")
+    x[6, 2] = y[6, 2] = 0
+    gain[2] = float("nan")
+    check_norm(x, y, gain, 1e-6, "gain NaN")
+
+
+# ---------------------------------------------------------------------------
+# Codes of rows and of gated activations
+# ---------------------------------------------------------------------------
+
+def check_quant(x, up, act, tag):
+    rows, d = x.shape
+    q, whole = guarded_q8(rows, d)
+    assert prox.quant_q8(x, up, act, q=q) is q and (whole[:, d:] == 77).all(), tag
+    c, s = R.codes(f64(x) if up is None else R.act(f64(x), f64(up), act))
+    R.check_codes(q.codes, c, tag)
+    R.check_scales(q.scales, s, tag)
+    values = prox.read_q8(q)
+    want = q.codes.float() * q.scales[:, None]
+    assert torch.equal(values.view(torch.int32)[torch.isfinite(want)], want.view(torch.int32)[torch.isfinite(want)])
+    assert torch.equal(torch.isnan(values), torch.isnan(want))
+    return q
+
+
+ACTS = [None, prox.SILU, prox.GELU]
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_quant_widths(d, dtype, act):
+    rows = 3
+    check_quant(randn((rows, d), d, dtype, 1.5), None if act is None else randn((rows, d), d + 1, dtype), act or 0, f"{d}")
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("rows", [1, 2, 5, 64, 256, 1030])
+def test_quant_rows(rows, act):
+    check_quant(randn((rows, 700), rows, BF16, 3.0), None if act is None else randn((rows, 700), 2, BF16), act or 0, f"{rows}")
+
+
+@pytest.mark.parametrize("act", [prox.SILU, prox.GELU])
+@pytest.mark.parametrize("d", [96, 1001, 4096])
+def test_halves_of_a_fused_projection(d, act):
+    # gate and up side by side, as one projection leaves them: the second half may start anywhere
+    x = randn((37, 2 * d), d, F16, 2.0)
+    got = prox.quant_q8(x[:, :d], x[:, d:], act)
+    want = prox.quant_q8(x[:, :d].contiguous(), x[:, d:].contiguous(), act)
+    assert torch.equal(got.codes, want.codes) and torch.equal(got.scales, want.scales)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("act", [prox.SILU, prox.GELU])
+def test_every_gate(dtype, act):
+    # Every finite 16-bit gate, and ups that bring its code next to a border: rows of up to 65536 gates.
+    g = torch.arange(-32768, 32768, dtype=torch.int32).to(torch.int16).view(dtype)
+    g = g[torch.isfinite(g)]
+    near = g[(g.abs() < 128)]
+    rows = [near[i::8][None] for i in range(8)]
+    for i, r in enumerate(rows):
+        x = r.cuda()
+        check_quant(x, torch.ones_like(x), act, f"part {i}")
+        check_quant(x, randn(x.shape, i, dtype), act, f"part {i}, random")
+        check_quant(-x.abs(), randn(x.shape, i, dtype), act, f"part {i}, negative gates")
+    check_quant(g[None].cuda(), torch.full((1, len(g)), 0.5, dtype=dtype, device="cuda"), act, "all")
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("d", [96, 1500, 9000])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_quant_extremes(d, dtype, act):
+    limit = 6e4 if dtype == F16 else 3.3e38
+    x = torch.from_numpy(np.stack([np.clip(f(d), -limit, limit) for f in EXTREMES.values()])).to(dtype).cuda()
+    if act is None:
+        check_quant(x, None, 0, "x")
+        return
+    for up in (1.0, -0.37, 1e-5, 3e4):
+        check_quant(x, torch.full_like(x, up), act, f"up {up}")
+    if dtype == BF16:
+        check_quant(x, torch.full_like(x, 1e30), act, "up 1e30")
+        check_quant(torch.full_like(x, -84.0), randn(x.shape, 1, dtype, 1e36), act, "far negative gates")
+    check_quant(torch.full_like(x, -20.0), randn(x.shape, 1, dtype), act, "negative gates")
+    check_quant(torch.zeros_like(x), randn(x.shape, 1, dtype), act, "gates of 0")
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("d", [96, 1500, 9000])
+def test_quant_not_finite(d, act):
+    x, u = randn((7, d), 1, BF16), randn((7, d), 2, BF16)
+    x[1, 5], x[2, d - 1], u[3, 0], u[4, 9] = float("nan"), float("inf"), float("nan"), float("inf")
+    x[5, 2] = -float("inf")
+    q = check_quant(x, None if act is None else u, act or 0, "")
+    assert not torch.isnan(q.scales[[0, 6]]).any() and torch.isnan(q.scales[[1, 2, 5]]).all()
+    if act is not None:
+        assert torch.isnan(q.scales[[3, 4]]).all()
+
+
+def test_read_of_odd_rows():
+    for rows, d in ((1, 1), (3, 5), (7, 33), (2, 4097), (300, 1000)):
+        q, _ = guarded_q8(rows, d)
+        q.codes.copy_(torch.randint(-128, 128, (rows, d), generator=torch.Generator().manual_seed(d)))
+        q.scales.copy_(randn((rows,), 1, torch.float32))
+        assert torch.equal(prox.read_q8(q), q.codes.float() * q.scales[:, None])
+
+
+def test_no_rows_is_no_work():
+    x = torch.empty((0, 64), dtype=BF16, device="cuda")
+    assert prox.rmsnorm(x).shape == (0, 64) and prox.quant_q8(x).codes.shape == (0, 64)
+    assert prox.read_q8(prox.rmsnorm_q8(x)).shape == (0, 64)
+
+
+def test_refusals_on_the_device():
+    x = randn((4, 64), 1, BF16)
+    with pytest.raises(prox.ProxError):
+        prox.rmsnorm(x, out=x, residual=x)
+    with pytest.raises(prox.ProxError):
+        prox.rmsnorm(x, eps=-1.0)
+    with pytest.raises(prox.ProxError):
+        prox.quant_q8(x, x, act=7)
+    with pytest.raises(prox.ProxError):
+        prox.quant_q8(x[:1].expand(4, 64))                     # rows on top of each other
+    with pytest.raises(ValueError):
+        prox.quant_q8(x, x[:3])
+    with pytest.raises(ValueError):
+        prox.rmsnorm(x, gain=x[0, :63])
+    with pytest.raises(ValueError):
+        prox.rmsnorm(x, y=x.half())
+    with pytest.raises(ValueError):
+        prox.rmsnorm_q8(x, q=prox.new_rows_q8(4, 65))
+    with pytest.raises(ValueError):
+        prox.rmsnorm_q8(x.t())
+    q = prox.new_rows_q8(4, 64)
+    with pytest.raises(ValueError):
+        prox.read_q8(prox.RowsQ8(q.codes, q.scales[:3]))
+    with pytest.raises(prox.ProxError):
+        prox.read_q8(prox.RowsQ8(torch.zeros((4, 65), dtype=torch.int8, device="cuda"), q.scales))   # rows 65 bytes apart
+
+
+@pytest.mark.parametrize("d", [300, 1500, 9000])
+def test_capture_and_streams(d):
+    x, y, gain, up = (randn((40, d), i, BF16) for i in (1, 2, 3, 4))
+    gain = gain[0].clone()
+    q, s, out, r = prox.new_rows_q8(40, d), prox.new_rows_q8(40, d), torch.empty_like(x), torch.empty_like(x)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        prox.rmsnorm_q8(x, y, gain, residual=r, out=out, q=q)
+        prox.quant_q8(out, up, prox.SILU, q=s)
+    other = torch.cuda.Stream()
+    for seed in range(3):
+        x.copy_(hidden(40, d, seed, BF16))
+        g.replay()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            want_out = torch.empty_like(x)
+            want = prox.rmsnorm_q8(x, y, gain, out=want_out)
+            want_s = prox.quant_q8(want_out, up, prox.SILU)
+        other.synchronize()
+        assert torch.equal(q.codes, want.codes) and torch.equal(q.scales, want.scales) and torch.equal(out, want_out)
+        assert torch.equal(s.codes, want_s.codes) and torch.equal(s.scales, want_s.scales)
+        assert torch.equal(r, (x.float() + y.float()).to(BF16))
+
+
+def test_offsets_past_32_bits():
+    # The last rows stand past 2^32 bytes of the first.
+    rows, d = 40, 64
+    pitch = 1 << 27
+    x = torch.empty_strided((rows, d), (pitch, 1), dtype=BF16, device="cuda")
+    codes = torch.empty_strided((rows, d), (pitch, 1), dtype=torch.int8, device="cuda")
+    x.copy_(hidden(rows, d, 1, BF16))
+    q = prox.RowsQ8(codes, torch.empty(rows, device="cuda"))
+    prox.quant_q8(x, q=q)
+    want = prox.quant_q8(x.contiguous())
+    assert torch.equal(q.codes, want.codes) and torch.equal(prox.read_q8(q), prox.read_q8(want))
+    out = torch.empty_strided((rows, d), (pitch, 1), dtype=BF16, device="cuda")
+    assert torch.equal(prox.rmsnorm(x, x, out=out), prox.rmsnorm(x.contiguous(), x.contiguous()))
