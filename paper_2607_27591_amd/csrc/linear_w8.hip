@@ -1,5 +1,10 @@
 // Projections on 8-bit integers, y = (c_x c_w^T) sigma_x sigma_w (+ bias): weights packed and unpacked, and
-// the product.
+// the product: y^T = W x^T as 16 x 16 x 64 MFMAs, exact in 32 bits.  The weights go from the caches to registers as
+// operands (every wave's outputs are its own, and their layout is the operands'), x through LDS, where the waves share it;
+// the sums are scaled and rounded once.  Few rows are bound by the weights' bytes (28672 x 8192, 16 rows 38.4 us,
+// 6.1 TB/s), many by power: at 4096 rows the clock falls to 1.8 GHz (715 us, 2690 TOP/s).  What saves power there:
+// 16 x 16 x 64 products rather than 32 x 32 x 32 (random operands, nothing else: 3695 and 3160 TOP/s), one operand
+// kept from product to product (4075 TOP/s).
 #include "linear_w8.hpp"
 
 namespace prox {
@@ -60,33 +65,259 @@ __global__ __launch_bounds__(256) void unpack_w8_kernel(const uint8_t *__restric
     }
 }
 
-// A wave takes 64 outputs of 16 rows over all inputs.
+// Two values rounded to the dtype (NaN stays NaN).
 template <int DT>
-__global__ __launch_bounds__(256) void linear_w8_kernel(Linear8Args A) {
-    const Linear8Layout L(A.n, A.k);
-    const int wave = threadIdx.x / kWave, lane = lane_id(), h = lane / 16, col = lane % 16;
-    const int groups = (L.nblocks + 3) / 4;
-    const int nb = (int)(blockIdx.x % groups) * 4 + wave, row = (int)(blockIdx.x / groups) * 16 + col;
-    if (nb >= L.nblocks) return;
-    const int8_t *x = A.x + (size_t)min(row, A.rows - 1) * A.ldx;
-    const uint8_t *w = A.blob + (size_t)nb * L.kblocks * 4096 + lane * 16;
-    v4i acc[4] = {};
-    for (int b = 0; b < L.kblocks; ++b) {
-        const int i = 64 * b + 16 * h;
-        v4i xv = {0, 0, 0, 0};
-        if (i < A.k) xv = *reinterpret_cast<const v4i *>(x + i);   // up to 15 bytes past k, times codes 0
+__device__ __forceinline__ uint32_t to_pair(float a, float b) {
+    if constexpr (DT == kBF16) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+    else return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+}
+
+// Weights that are read once by a call (ONCE) are loaded as a stream: 28672 x 8192, 16 rows 38.4 us, without 44.6.
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load_weights(const uint8_t *p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+    else return *reinterpret_cast<const u32x4 *>(p);
+}
+
+// Four outputs from j of a row: scales, bias and rounding.
+template <int DT>
+__device__ __forceinline__ uint2 finish4(const Linear8Args &A, const float *ws, int j, float sx, v4i acc) {
+    const v4f sw = *reinterpret_cast<const v4f *>(ws + j);   // padded to 64 outputs
+    float v[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) acc[t] = mfma16_i8(*reinterpret_cast<const v4i *>(w + (size_t)b * 4096 + t * 1024), xv, acc[t]);
+    for (int e = 0; e < 4; ++e) v[e] = fmaf((float)acc[e] * sw[e], sx, A.bias ? half_to_float<DT>(A.bias[min(j + e, A.n - 1)]) : 0.0f);
+    return make_uint2(to_pair<DT>(v[0], v[1]), to_pair<DT>(v[2], v[3]));
+}
+
+// W8Shape: a wave takes 16 NT outputs by 16 MT rows; a workgroup WN x WM waves, WK times: its WK parts take a step of
+// 128 inputs in turn.  S: halves of a step whose weights are in registers or on the way; XD: steps of x alike.
+template <int NT_, int MT_, int WM_, int WN_, int WK_, int S_, int XD_>
+struct W8Shape {
+    static constexpr int NT = NT_, MT = MT_, WM = WM_, WN = WN_, WK = WK_, S = S_, XD = XD_;
+    static constexpr int OUTS = 16 * NT * WN, ROWS = 16 * MT * WM, PART = 64 * WM * WN, THREADS = PART * WK;
+    static constexpr int XL = ROWS * 8 / PART;                     // loads of x of a step by each of its threads
+    static constexpr int PM = MT < 4 ? MT : 4, PH = MT / PM;       // row fragments of a phase, phases of a half
+    static constexpr int U = S % 2 ? S : S / 2 > XD ? S / 2 : XD;  // steps until the sets of registers stand as before
+    static constexpr int WAVES = THREADS / 64;
+    static constexpr int MC = WAVES * NT * MT <= 128 ? MT : 128 / (WAVES * NT);   // row fragments whose parts are added at a time
+    static constexpr bool TILE = NT == 4 && (WK == 1 || MC % WK == 0);   // whole rows of 64 outputs are written through LDS
+    static constexpr int MINE = WK == 1 ? (MT < 4 ? MT : 4) : MC / WK;   // row fragments of a part at a time, then
+    static constexpr size_t stage = (size_t)2 * WK * ROWS * 128;
+    static constexpr size_t last = WK == 1 ? (size_t)WAVES * MINE * 2048 : (size_t)WAVES * NT * MC * 1024;
+    static constexpr size_t lds = stage > last ? stage : last;
+    static_assert(XL * PART == ROWS * 8 && PM * PH == MT && (2 * U) % S == 0 && U % XD == 0, "whole loads, phases and turns");
+    static_assert(lds <= 163840 && MT % MC == 0 && (TILE || MC == MT), "LDS");
+};
+
+// ONCE: no two workgroups read the same weights.
+template <int DT, class C, bool ONCE>
+__global__ __launch_bounds__(C::THREADS, (C::THREADS + 511) / 512 * 2) void linear_w8_kernel(Linear8Args A, int mtiles, int ntiles) {
+    constexpr int NT = C::NT, MT = C::MT, WM = C::WM, WN = C::WN, WK = C::WK, S = C::S, XD = C::XD, ROWS = C::ROWS, XL = C::XL;
+    constexpr int PM = C::PM, PH = C::PH, U = C::U, H = 2 * U;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const Linear8Layout L(A.n, A.k);
+    // Workgroups go round the 8 XCDs: each takes a run of tiles, 4 row tiles deep.
+    const int total = mtiles * ntiles, id = (int)blockIdx.x, q = total / 8, rem = total % 8;
+    const int xcd = id % 8, at = xcd * q + min(xcd, rem) + id / 8;
+    const int group = at / (4 * ntiles), depth = min(4, mtiles - 4 * group), in = at - group * 4 * ntiles;
+    const int row0 = (4 * group + in % depth) * ROWS, ntile = in / depth;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = lane_id();
+    const int part = wave / (WM * WN), wm = wave % WM, wn = wave / WM % WN, h = lane / 16, col = lane % 16;
+    const int pt = (int)threadIdx.x % C::PART;
+    const int tile0 = (ntile * WN + wn) * NT;   // of 16 outputs
+    const uint8_t *w = A.blob + (size_t)min(tile0 / 4, L.nblocks - 1) * L.kblocks * 4096 + tile0 % 4 * 1024;
+    v4i *xs = reinterpret_cast<v4i *>(smem) + part * 2 * ROWS * 8;   // [buffer][row][chunk of 16 inputs ^ row % 8]
+    // Rows past the last: the last again (not stored).  Inputs past k: any, they meet codes 0.
+    const int8_t *x = A.x + (size_t)row0 * A.ldx;
+    const int chunk = pt % 8, kend = (A.k - 1) / 16 * 16;
+    int xrow[XL];
+#pragma unroll
+    for (int l = 0; l < XL; ++l) xrow[l] = min(l * (C::PART / 8) + pt / 8, A.rows - 1 - row0) * (int)A.ldx;
+    const int xst = (pt / 8) * 8 + (chunk ^ (pt / 8 % 8));
+    const int ksteps = L.kblocks / 2, steps = (ksteps + WK - 1) / WK;   // step i of this part: inputs from 128 (i WK + part)
+    v4i acc[NT][MT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[t][m] = v4i{0, 0, 0, 0};
+    v4i xv[XD][XL], wv[S][NT], b[2][PM];
+    auto load_x = [&](int set, int l, int i) {
+        xv[set][l] = *reinterpret_cast<const v4i *>(x + (uint32_t)(xrow[l] + min((min(i, steps - 1) * WK + part) * 128 + chunk * 16, kend)));
+    };
+    auto store_x = [&](int set, int l, int i) {
+        v4i v = xv[set][l];
+        if (WK > 1 && i * WK + part >= ksteps) v = v4i{0, 0, 0, 0};   // past the last step of all: weights of another meet zeros
+        xs[(i % 2) * ROWS * 8 + l * C::PART + xst] = v;
+    };
+    auto load_w = [&](int set, int t, int i) {   // half i
+        const int k = min(2 * (min(i / 2, steps - 1) * WK + part) + i % 2, L.kblocks - 1);
+        wv[set][t] = __builtin_bit_cast(v4i, load_weights<ONCE>(w + (size_t)k * 4096 + (uint32_t)(lane * 16 + t * 1024)));
+    };
+    auto read_b = [&](int p, int m, int buf) {
+        const int row = (wm * MT + p % PH * PM + m) * 16 + col;
+        b[p % 2][m] = xs[buf * ROWS * 8 + row * 8 + ((4 * (p / PH) + h) ^ (col % 8))];
+    };
+    auto part_sync = [&] {
+        if constexpr (WM * WN == 1) wave_lds_fence();   // x is this wave's own: LDS serves it in order
+        else __syncthreads();
+    };
+    // Loads are counted in order: those in flight before the first step stand as they do before every other.
+#pragma unroll
+    for (int l = 0; l < XL; ++l) load_x(0, l, 0);
+#pragma unroll
+    for (int l = 0; l < XL; ++l) store_x(0, l, 0);
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) {
+#pragma unroll
+        for (int d = 1; d <= XD; ++d)
+            if (i == (S - 2 - 2 * (XD - d) > 0 ? S - 2 - 2 * (XD - d) : 0)) {
+#pragma unroll
+                for (int l = 0; l < XL; ++l) load_x(d % XD, l, d);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) load_w(i, t, i);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    if (row >= A.rows) return;
-    const float *ws = reinterpret_cast<const float *>(A.blob + L.scales);
-    const float xs = A.scales[row];
-    for (int t = 0; t < 4; ++t)
-        for (int e = 0; e < 4; ++e) {
-            const int j = nb * kLinear8N + w8_output(t, 4 * h + e);
-            if (j < A.n)
-                A.y[(size_t)row * A.ldy + j] = to_half<DT>(fmaf((float)acc[t][e] * ws[j], xs, A.bias ? half_to_float<DT>(A.bias[j]) : 0.0f));
+    part_sync();
+#pragma unroll
+    for (int m = 0; m < PM; ++m) read_b(0, m, 0);
+    for (int i0 = 0; i0 < steps; i0 += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u, buf = i % 2;
+            if (i >= steps) break;
+#pragma unroll
+            for (int p = 0; p < 2 * PH; ++p) {
+                // The operands of the next phase; those of the next step are there behind the barrier.
+                if (p == 2 * PH - 1) part_sync();
+                const int half = 2 * u + p / PH;
+#pragma unroll
+                for (int m = 0; m < PM; ++m) {
+                    // Reads, loads and stores between the products, which leave 12 of 16 cycles to them.  Past the last
+                    // step: the last again, unused (no branches, which would cost the count of loads in flight).
+                    read_b((p + 1) % (2 * PH), m, p == 2 * PH - 1 ? buf ^ 1 : buf);
+                    if (p % PH == 0) {   // into the set of the half before, of which no product is left
+#pragma unroll
+                        for (int t = m * NT / PM; t < (m + 1) * NT / PM; ++t) load_w((half + H - 1) % S, t, 2 * i + p / PH + S - 1);
+                    }
+                    if (p == (PH > 1)) {
+#pragma unroll
+                        for (int l = m * XL / PM; l < (m + 1) * XL / PM; ++l) {
+                            store_x((u + 1) % XD, l, i + 1);
+                            load_x((u + 1) % XD, l, i + 1 + XD);
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int e = 0; e < NT; ++e) {   // one operand of two stays from product to product: less power, a higher clock
+                        const int t = m % 2 ? NT - 1 - e : e;
+                        acc[t][p % PH * PM + m] = mfma16_i8(wv[half % S][t], b[p % 2][m], acc[t][p % PH * PM + m]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         }
+    }
+    const float *ws = reinterpret_cast<const float *>(A.blob + L.scales);
+    v4i *red = reinterpret_cast<v4i *>(smem);   // [wave][row fragment][tile][lane]
+    // The parts' sums of row fragments m0 .. m0 + MC - 1, to LDS; and of tile (t, m0 + m) of this wave's outputs and rows.
+    auto share = [&](int m0) {
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < C::MC; ++m)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) red[((wave * C::MC + m) * NT + t) * kWave + lane] = acc[t][m0 + m];
+        __syncthreads();
+    };
+    auto sum = [&](int t, int m) {
+        v4i s{0, 0, 0, 0};
+#pragma unroll
+        for (int g = 0; g < WK; ++g) s += red[(((g * WM * WN + wave % (WM * WN)) * C::MC + m) * NT + t) * kWave + lane];
+        return s;
+    };
+    const int row1 = row0 + wm * MT * 16;
+    if constexpr (C::TILE) {   // this part's row fragments, MINE at a time
+        constexpr int MINE = C::MINE, EACH = MINE * WK;
+        const int j0 = tile0 * 16;
+        const bool whole = j0 + 64 <= A.n;
+        v4i *out = reinterpret_cast<v4i *>(smem) + wave * MINE * 128;
+#pragma unroll
+        for (int m0 = 0; m0 < MT; m0 += EACH) {
+            v4i v[4][MINE];
+            if constexpr (WK > 1) share(m0);
+#pragma unroll
+            for (int f = 0; f < MINE; ++f)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) v[t][f] = WK > 1 ? sum(t, part * MINE + f) : acc[t][m0 + f];
+            if constexpr (WK > 1) __syncthreads();
+            else wave_lds_fence();
+            if (j0 >= A.n) continue;
+            const int first = row1 + (m0 + part * MINE) * 16;
+#pragma unroll
+            for (int f = 0; f < MINE; ++f) {
+                const float sx = A.scales[min(first + 16 * f + col, A.rows - 1)];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {   // outputs 16 h + 8 c .. + 7
+                    const uint2 lo = finish4<DT>(A, ws, j0 + 16 * h + 8 * c, sx, v[2 * c][f]);
+                    const uint2 hi = finish4<DT>(A, ws, j0 + 16 * h + 8 * c + 4, sx, v[2 * c + 1][f]);
+                    out[f * 128 + col * 8 + ((2 * h + c) ^ (col % 8))] = v4i{(int)lo.x, (int)lo.y, (int)hi.x, (int)hi.y};
+                }
+            }
+            wave_lds_fence();
+#pragma unroll
+            for (int l = 0; l < 2 * MINE; ++l) {   // 8 lanes write the 128 bytes of a row
+                const int r = 8 * l + lane / 8, c = lane % 8;
+                if (first + r >= A.rows) continue;
+                const v4i o = out[r * 8 + (c ^ (r % 8))];
+                uint16_t *dst = A.y + (size_t)(first + r) * A.ldy + j0 + 8 * c;
+                if (whole) {
+                    __builtin_memcpy(__builtin_assume_aligned(dst, 2), &o, 16);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (j0 + 8 * c + e < A.n) dst[e] = (uint16_t)((uint32_t)o[e / 2] >> (16 * (e % 2)));
+                }
+            }
+        }
+    } else {   // tiles in turn among the parts
+        share(0);
+        for (int v = part; v < NT * MT; v += WK) {
+            const int t = v % NT, m = v / NT, row = row1 + 16 * m + col;
+            const int j = (tile0 + t) / 4 * kLinear8N + w8_output((tile0 + t) % 4, 4 * h);
+            if (row >= A.rows || j >= A.n) continue;
+            const uint2 o = finish4<DT>(A, ws, j, A.scales[row], sum(t, m));
+            uint16_t *dst = A.y + (size_t)row * A.ldy + j;
+            if (j + 4 <= A.n) {
+                __builtin_memcpy(__builtin_assume_aligned(dst, 2), &o, 8);
+            } else {
+                dst[0] = (uint16_t)o.x;
+                if (j + 1 < A.n) dst[1] = (uint16_t)(o.x >> 16);
+                if (j + 2 < A.n) dst[2] = (uint16_t)o.y;
+            }
+        }
+    }
+}
+
+template <int DT, class C, bool ONCE>
+hipError_t run_once(const Linear8Args &a, hipStream_t s) {
+    auto *kernel = linear_w8_kernel<DT, C, ONCE>;
+    if constexpr (C::lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::lds);
+        if (e != hipSuccess) return e;
+    }
+    // The outputs of a block of 64 are spread over its four tiles: all of them are needed.
+    const int mtiles = (a.rows + C::ROWS - 1) / C::ROWS, ntiles = ((a.n + 63) / 64 * 64 + C::OUTS - 1) / C::OUTS;
+    kernel<<<(unsigned)(mtiles * ntiles), C::THREADS, C::lds, s>>>(a, mtiles, ntiles);
+    return hipGetLastError();
+}
+
+template <int DT, class C>
+hipError_t run(const Linear8Args &a, hipStream_t s) {
+    if constexpr (C::ROWS <= 64) {
+        if (a.rows <= C::ROWS) return run_once<DT, C, true>(a, s);
+    }
+    return run_once<DT, C, false>(a, s);
 }
 
 }  // namespace
@@ -106,12 +337,50 @@ hipError_t launch_unpack_linear_w8(const void *blob, int n, int k, int8_t *codes
     return hipGetLastError();
 }
 
+// The variant by shape: the one whose rounds of 256 workgroups (one a CU) take least, by the time of a round: its start and
+// last step, and 1024 inputs.  Larger tiles read less from the L2 for each product, which bounds all but the
+// largest; smaller ones fill the CUs.  In us at k = 4096 (bf16, streams of calls), for 1 round and for 4:
+//   256 x 256  59.8, 227    128 x 256  34.2, 142    128 x 128  22.0, 84    64 x 256  21.7, 96    64 x 128  14.2, 53
+//   32 x 128   11.3, 41     64 x 64    11.2, 39     32 x 64    8.3, 28     32 x 32   7.1, 17     16 x 64   7.1, 20.5
+//   16 x 32    7.1, 13      16 x 16    7.1, 9.6
+// 512 rows, 6144 x 4096: 128 x 128 19.1, 64 x 128 25.5, 128 x 256 25.4, 256 x 256 40.8.  128 rows, 4096 x 4096: 32 x 64
+// 8.3, 32 x 32 10.0, 64 x 64 11, 128 x 128 17.6.  64 rows, 28672 x 8192: 64 x 128 41.6, 32 x 128 58.6, 64 x 64 55.
+struct W8Cost {
+    int rows, outs;
+    float start, k1024;   // us
+};
+constexpr W8Cost kW8Cost[] = {{256, 256, 5.7f, 12.8f}, {128, 256, 4.3f, 7.8f}, {128, 128, 5.7f, 3.83f}, {64, 256, 4.0f, 5.0f},
+                              {64, 128, 4.0f, 2.3f},   {32, 128, 3.3f, 1.73f}, {64, 64, 4.0f, 1.43f},   {32, 64, 3.05f, 1.0f},
+                              {32, 32, 2.5f, 0.46f},   {16, 64, 1.9f, 0.8f},   {16, 32, 1.7f, 0.4f},    {16, 16, 1.2f, 0.3f}};
+
+template <int DT>
+hipError_t launch_dt(const Linear8Args &a, hipStream_t s) {
+    int best = 0;
+    float least = 0.0f;
+    for (int v = 0; v < (int)(sizeof(kW8Cost) / sizeof(kW8Cost[0])); ++v) {
+        const W8Cost &c = kW8Cost[v];
+        const long long tiles = ((long long)a.rows + c.rows - 1) / c.rows * ((a.n + c.outs - 1) / c.outs);
+        const float t = (float)((tiles + 255) / 256) * (c.start + c.k1024 * (float)a.k / 1024.0f);
+        if (v == 0 || t < least) best = v, least = t;
+    }
+    switch (best) {
+    case 0: return run<DT, W8Shape<4, 8, 2, 4, 1, 3, 1>>(a, s);
+    case 1: return run<DT, W8Shape<4, 8, 1, 4, 2, 3, 1>>(a, s);
+    case 2: return run<DT, W8Shape<4, 4, 2, 2, 2, 4, 2>>(a, s);
+    case 3: return run<DT, W8Shape<4, 4, 1, 4, 2, 4, 2>>(a, s);
+    case 4: return run<DT, W8Shape<4, 4, 1, 2, 4, 4, 2>>(a, s);
+    case 5: return run<DT, W8Shape<4, 2, 1, 2, 4, 4, 2>>(a, s);
+    case 6: return run<DT, W8Shape<4, 4, 1, 1, 8, 4, 1>>(a, s);
+    case 7: return run<DT, W8Shape<4, 2, 1, 1, 8, 4, 2>>(a, s);
+    case 8: return run<DT, W8Shape<2, 2, 1, 1, 8, 4, 2>>(a, s);
+    case 9: return run<DT, W8Shape<4, 1, 1, 1, 8, 4, 2>>(a, s);
+    case 10: return run<DT, W8Shape<2, 1, 1, 1, 8, 4, 2>>(a, s);
+    default: return run<DT, W8Shape<1, 1, 1, 1, 8, 4, 2>>(a, s);
+    }
+}
+
 hipError_t launch_linear_w8(int dtype, const Linear8Args &a, hipStream_t s) {
-    const Linear8Layout L(a.n, a.k);
-    const unsigned grid = (unsigned)((L.nblocks + 3) / 4) * (unsigned)((a.rows + 15) / 16);
-    if (dtype == kBF16) linear_w8_kernel<kBF16><<<grid, 256, 0, s>>>(a);
-    else linear_w8_kernel<kF16><<<grid, 256, 0, s>>>(a);
-    return hipGetLastError();
+    return dtype == kBF16 ? launch_dt<kBF16>(a, s) : launch_dt<kF16>(a, s);
 }
 
 }  // namespace prox
