@@ -220,7 +220,7 @@ prox_status prox_rmsnorm_q8(const void *x, int64_t ldx, const void *y, int64_t l
         if (o && rows > 1 && ((o == x && (o == r ? ldr : ldo) != ldx) || (o == y && (o == r ? ldr : ldo) != ldy)))
             return PROX_ERR_INVALID;
     const NormArgs a{static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(y), static_cast<const uint16_t *>(gain),
-                     static_cast<uint16_t *>(r), static_cast<uint16_t *>(out), codes, scales, ldx, ldy, ldr, ldo, ldc, rows, d, eps};
+                     static_cast<uint16_t *>(r), static_cast<uint16_t *>(out), codes, scales, ldx, ldy, ldr, ldo, ldc, rows, d, eps, 1.0 / d};
     return hip_status(launch_rmsnorm_q8(dtype, a, stream));
 }
 

@@ -7,7 +7,7 @@
 
 namespace prox {
 
-enum { kActSilu = 0, kActGelu = 1, kActNone = 2 };
+enum { kActSilu = 0, kActGelu = 1 };
 
 struct NormArgs {
     const uint16_t *x, *y, *gain;   // y, gain may be NULL
@@ -17,6 +17,7 @@ struct NormArgs {
     int64_t ldx, ldy, ldr, ldo, ldc;
     int rows, d;
     float eps;
+    double inv_d;   // 1 / d
 };
 struct QuantArgs {
     const uint16_t *x, *up;   // up NULL: codes of x

@@ -887,22 +887,27 @@ def kv_attn(c: KVCache, s: KVSeqs, q: torch.Tensor, scale: Optional[float] = Non
 # ---------------------------------------------------------------------------
 
 @dataclasses.dataclass(frozen=True)
-class RowsQ8:
+class RowsQ8(_Handle):
     """Rows in 8 bits: device codes int8 [rows][d], whose rows stand a multiple of 16 bytes apart, and scales
     float32 [rows]; row b stands for scales[b] * codes[b].  Some of the rows: RowsQ8(q.codes[a:b], q.scales[a:b])."""
     codes: torch.Tensor
     scales: torch.Tensor
 
-    def check(self):
-        """(rows, d, row stride)."""
-        c, s = self.codes, self.scales
-        if c.dim() != 2:
-            raise ValueError("codes must be [rows][d]")
-        rows, ld = _rows2(c, "codes", torch.int8, c.shape[1])
-        _dev_tensor(s, "scales", torch.float32)
-        if tuple(s.shape) != (rows,):
-            raise ValueError("scales must be [rows]")
-        return rows, c.shape[1], ld
+    def parts(self):
+        """(rows, d, row stride, codes, scales, device index), as a call takes them."""
+        kept, c, s = self._kept, self.codes, self.scales
+        key = (c.data_ptr(), s.data_ptr(), c.shape)
+        if kept is None or kept[0] != key:
+            if c.dim() != 2:
+                raise ValueError("codes must be [rows][d]")
+            rows, ld = _rows2(c, "codes", torch.int8, c.shape[1])
+            _dev_tensor(s, "scales", torch.float32)
+            if tuple(s.shape) != (rows,):
+                raise ValueError("scales must be [rows]")
+            _same_device(c.device, s)
+            kept = (key, (rows, c.shape[1], ld, key[0], key[1], c.get_device()))
+            object.__setattr__(self, "_kept", kept)
+        return kept[1]
 
 
 def new_rows_q8(rows: int, d: int, device="cuda") -> RowsQ8:
@@ -912,56 +917,65 @@ def new_rows_q8(rows: int, d: int, device="cuda") -> RowsQ8:
 
 
 def _rows16(x: torch.Tensor, what: str):
-    """(rows, d, row stride) of 16-bit rows [rows][d], or [d]."""
-    if not isinstance(x, torch.Tensor) or x.dtype not in _TORCH_DT:
+    """(rows, d, row stride, C dtype) of 16-bit rows [rows][d], or [d]."""
+    dt = _TORCH_DT.get(x.dtype) if isinstance(x, torch.Tensor) else None
+    if dt is None:
         raise ValueError(f"{what} must be float16 or bfloat16")
-    if not 1 <= x.dim() <= 2:
+    shape = x.shape
+    if not 1 <= len(shape) <= 2:
         raise ValueError(f"{what} must be [rows][d]")
-    rows, ld = _rows2(x, what, x.dtype, x.shape[-1])
-    return rows, x.shape[-1], ld
+    rows, ld = _rows2(x, what, x.dtype, shape[-1])
+    return rows, shape[-1], ld, dt
 
 
-def _like(t: Optional[torch.Tensor], what: str, x: torch.Tensor, rows: int, d: int) -> int:
-    """Row stride of t, which has x's rows (0 without t)."""
-    if t is None:
-        return 0
+def _like(t: torch.Tensor, what: str, x: torch.Tensor, rows: int, d: int, ldx: int) -> int:
+    """Row stride of t, which has x's rows, type and device."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != x.get_device():
+        raise ValueError(f"{what} must be a tensor on the device of x")
+    if t.shape == x.shape and t.dtype == x.dtype and t.stride() == x.stride():
+        return ldx
     n, ld = _rows2(t, what, x.dtype, d)
     if n != rows:
         raise ValueError(f"{what} must have the rows of x")
     return ld
 
 
-def _q8_out(q: Optional[RowsQ8], rows: int, d: int, device):
-    """(q, row stride): rows to write to, made when not given."""
-    q = new_rows_q8(rows, d, device) if q is None else q
-    n, w, ld = q.check()
-    if (n, w) != (rows, d):
-        raise ValueError("q must have the shape of x")
-    return q, ld
+def _q8_like(q: RowsQ8, x: torch.Tensor, rows: int, d: int):
+    """(row stride, codes, scales) of q, which takes x's rows."""
+    n, w, ld, codes, scales, index = q.parts()
+    if n != rows or w != d or index != x.get_device():
+        raise ValueError("q must have the shape and the device of x")
+    return ld, codes, scales
 
 
-def _norm(x, y, gain, eps, residual, out, q):
-    rows, d, ldx = _rows16(x, "x")
-    ldy, ldr, ldo = (_like(t, n, x, rows, d) for t, n in ((y, "y"), (residual, "residual"), (out, "out")))
-    ldc = 0
+def _norm(x, rows, d, ldx, dt, y, gain, eps, residual, out, q):
+    ldy = ldr = ldo = ldc = 0
+    py = pr = po = pg = codes = scales = None
+    if y is not None:
+        ldy, py = _like(y, "y", x, rows, d, ldx), y.data_ptr()
+    if residual is not None:
+        ldr, pr = _like(residual, "residual", x, rows, d, ldx), residual.data_ptr()
+    if out is not None:
+        ldo, po = _like(out, "out", x, rows, d, ldx), out.data_ptr()
     if q is not None:
-        q, ldc = _q8_out(q, rows, d, x.device)
+        ldc, codes, scales = _q8_like(q, x, rows, d)
     if gain is not None:
         _dev_tensor(gain, "gain", x.dtype)
-        if gain.numel() != d:
-            raise ValueError("gain must be [d]")
-    codes, scales = (None, None) if q is None else (q.codes, q.scales)
-    _same_device(x.device, y, gain, residual, out, codes, scales)
-    _check(_on(x.device, lib().prox_rmsnorm_q8, x.data_ptr(), ldx, _at(y), ldy, _at(gain), rows, d, _TORCH_DT[x.dtype],
-               float(eps), _at(residual), ldr, _at(out), ldo, _at(codes), ldc, _at(scales)), "prox_rmsnorm_q8")
+        if gain.numel() != d or gain.get_device() != x.get_device():
+            raise ValueError("gain must be [d], on the device of x")
+        pg = gain.data_ptr()
+    _check(_on(x.device, lib().prox_rmsnorm_q8, x.data_ptr(), ldx, py, ldy, pg, rows, d, dt, eps, pr, ldr, po, ldo, codes,
+               ldc, scales), "prox_rmsnorm_q8")
 
 
 def rmsnorm(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
             residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Root-mean-square norm of the rows r = x + y (x without y), times gain [d], in their own type.  r, rounded to
     that type, goes to `residual` where given; residual or out may be x or y."""
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    _norm(x, y, gain, eps, residual, out, None)
+    rows, d, ldx, dt = _rows16(x, "x")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _norm(x, rows, d, ldx, dt, y, gain, eps, residual, out, None)
     return out
 
 
@@ -969,32 +983,34 @@ def rmsnorm_q8(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: Optional
                residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                q: Optional[RowsQ8] = None) -> RowsQ8:
     """rmsnorm with its result in 8 bits (q, made when not given), and in the rows' own type too where `out` is given."""
+    rows, d, ldx, dt = _rows16(x, "x")
     if q is None:
-        rows, d, _ = _rows16(x, "x")
         q = new_rows_q8(rows, d, x.device)
-    _norm(x, y, gain, eps, residual, out, q)
+    _norm(x, rows, d, ldx, dt, y, gain, eps, residual, out, q)
     return q
 
 
 def quant_q8(x: torch.Tensor, up: Optional[torch.Tensor] = None, act: int = SILU, q: Optional[RowsQ8] = None) -> RowsQ8:
     """Rows in 8 bits: of x, or of act(x) * up (SILU or GELU)."""
-    rows, d, ldx = _rows16(x, "x")
-    ldu = _like(up, "up", x, rows, d)
-    q, ldc = _q8_out(q, rows, d, x.device)
-    _same_device(x.device, up, q.codes, q.scales)
-    _check(_on(x.device, lib().prox_quant_q8, x.data_ptr(), ldx, _at(up), ldu, _int32(act), rows, d, _TORCH_DT[x.dtype],
-               q.codes.data_ptr(), ldc, q.scales.data_ptr()), "prox_quant_q8")
+    rows, d, ldx, dt = _rows16(x, "x")
+    ldu, pu = (0, None) if up is None else (_like(up, "up", x, rows, d, ldx), up.data_ptr())
+    if q is None:
+        q = new_rows_q8(rows, d, x.device)
+    ldc, codes, scales = _q8_like(q, x, rows, d)
+    _check(_on(x.device, lib().prox_quant_q8, x.data_ptr(), ldx, pu, ldu, _int32(act), rows, d, dt, codes, ldc, scales),
+           "prox_quant_q8")
     return q
 
 
 def read_q8(q: RowsQ8, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """What rows in 8 bits stand for: float32 [rows][d]."""
-    rows, d, ldc = q.check()
-    out = torch.empty((rows, d), dtype=torch.float32, device=q.codes.device) if out is None else _dev_tensor(out, "out", torch.float32)
-    if tuple(out.shape) != (rows, d):
-        raise ValueError("out must be [rows][d]")
-    _same_device(q.codes.device, q.scales, out)
-    _check(_on(out.device, lib().prox_read_q8, q.codes.data_ptr(), ldc, q.scales.data_ptr(), rows, d, out.data_ptr()), "prox_read_q8")
+    rows, d, ldc, codes, scales, index = q.parts()
+    if out is None:
+        out = torch.empty((rows, d), dtype=torch.float32, device=q.codes.device)
+    _dev_tensor(out, "out", torch.float32)
+    if out.shape != q.codes.shape or out.get_device() != index:
+        raise ValueError("out must be [rows][d], on the device of q")
+    _check(_on(out.device, lib().prox_read_q8, codes, ldc, scales, rows, d, out.data_ptr()), "prox_read_q8")
     return out
 
 
@@ -1045,22 +1061,23 @@ def unpack_linear_w8(q: LinearW8):
 
 def linear_w8(w: LinearW8, x: RowsQ8, bias: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rows in 8 bits times the INT8 weights, plus bias [n]: [rows][n] in the weights' type; rows of y may stand apart."""
-    rows, k, ldc = x.check()
+    rows, k, ldc, codes, scales, index = x.parts()
     if k != w.k:
         raise ValueError(f"x must be [rows][{w.k}]")
-    dev = x.codes.device
     if y is None:
-        y = torch.empty((rows, w.n), dtype=w.dtype, device=dev)
+        y = torch.empty((rows, w.n), dtype=w.dtype, device=x.codes.device)
     n, ldy = _rows2(y, "y", w.dtype, w.n)
     if n != rows:
         raise ValueError("y must have the rows of x")
+    pb = None
     if bias is not None:
         _dev_tensor(bias, "bias", w.dtype)
-        if bias.numel() != w.n:
-            raise ValueError("bias must be [n]")
-    _same_device(dev, w.blob, x.scales, y, bias)
-    _check(_on(dev, lib().prox_linear_w8, w.pointer(), x.codes.data_ptr(), ldc, x.scales.data_ptr(), rows, _at(bias),
-               y.data_ptr(), ldy), "prox_linear_w8")
+        if bias.numel() != w.n or bias.get_device() != index:
+            raise ValueError("bias must be [n], on the device of x")
+        pb = bias.data_ptr()
+    if y.get_device() != index or w.blob.get_device() != index:
+        raise ValueError("every tensor of a call must be on one device")
+    _check(_on(y.device, lib().prox_linear_w8, w.pointer(), codes, ldc, scales, rows, pb, y.data_ptr(), ldy), "prox_linear_w8")
     return y
 
 
