@@ -25,6 +25,8 @@ __device__ __forceinline__ void each(F f) {
     }
 }
 
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
 // 8 elements of a row that may start at any element; n of them (at least 1) where the row ends there (TAIL), else 0.
 template <bool TAIL>
 __device__ __forceinline__ uint4 load8(const uint16_t *p, int n) {
@@ -40,10 +42,14 @@ __device__ __forceinline__ uint4 load8(const uint16_t *p, int n) {
     }
     return v;
 }
-template <bool TAIL>
+// STREAM: past the caches' usual order, for what the next kernel does not read (the residual: norm of 2048 x 8192
+// 20.9 us, else 26.8; codes so would cost the projection behind them more than the norm gains).
+template <bool TAIL, bool STREAM>
 __device__ __forceinline__ void store8(uint16_t *p, int n, const uint4 &v) {
     if (!TAIL || n >= 8) {
-        __builtin_memcpy(__builtin_assume_aligned(p, 2), &v, 16);
+        const u32x4_any w{v.x, v.y, v.z, v.w};
+        if constexpr (STREAM) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any *>(p));
+        else *reinterpret_cast<u32x4_any *>(p) = w;
     } else {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -233,7 +239,7 @@ __global__ __launch_bounds__(C::threads) void rmsnorm_kernel(NormArgs A) {
     if (A.r) {
         each<CH>([&](auto c) {
             const int i = (c * T + t) * 8, n = d - i;
-            if (n > 0) store8<TAIL>(A.r + (size_t)row * A.ldr + i, n, r[c]);
+            if (n > 0) store8<TAIL, true>(A.r + (size_t)row * A.ldr + i, n, r[c]);
         });
     }
     each<CH>([&](auto c) {
@@ -268,7 +274,7 @@ __global__ __launch_bounds__(C::threads) void rmsnorm_kernel(NormArgs A) {
             if (A.out) {
                 const uint4 w = make_uint4(round_pair<DT>(p[0] * invf, p[1] * invf), round_pair<DT>(p[2] * invf, p[3] * invf),
                                            round_pair<DT>(p[4] * invf, p[5] * invf), round_pair<DT>(p[6] * invf, p[7] * invf));
-                store8<TAIL>(A.out + (size_t)row * A.ldo + i, n, w);
+                store8<TAIL, false>(A.out + (size_t)row * A.ldo + i, n, w);
             }
             if (A.codes) {
                 uint32_t near;
@@ -312,7 +318,7 @@ __global__ __launch_bounds__(C::threads) void rmsnorm_kernel(NormArgs A) {
             else o.w |= h;
             if (finite && most > 0.0) set_code(code, e, exact_code(p, most));
         }
-        if (A.out) store8<TAIL>(A.out + (size_t)row * A.ldo + i, n, o);
+        if (A.out) store8<TAIL, false>(A.out + (size_t)row * A.ldo + i, n, o);
         if (A.codes) store_codes<TAIL>(A.codes + (size_t)row * A.ldc + i, n, code);
     });
 }
