@@ -115,7 +115,7 @@ __global__ __launch_bounds__(C::THREADS, (C::THREADS + 511) / 512 * 2) void line
     constexpr int NT = C::NT, MT = C::MT, WM = C::WM, WN = C::WN, WK = C::WK, S = C::S, XD = C::XD, ROWS = C::ROWS, XL = C::XL;
     constexpr int PM = C::PM, PH = C::PH, U = C::U, H = 2 * U;
     extern __shared__ __align__(16) unsigned char smem[];
-    const Linear8Layout L(A.n, A.k);
+    const int nblocks = (A.n + kLinear8N - 1) / kLinear8N;
     // Workgroups go round the 8 XCDs: each takes a run of tiles, 4 row tiles deep.
     const int total = mtiles * ntiles, id = (int)blockIdx.x, q = total / 8, rem = total % 8;
     const int xcd = id % 8, at = xcd * q + min(xcd, rem) + id / 8;
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(C::THREADS, (C::THREADS + 511) / 512 * 2) void line
     const int part = wave / (WM * WN), wm = wave % WM, wn = wave / WM % WN, h = lane / 16, col = lane % 16;
     const int pt = (int)threadIdx.x % C::PART;
     const int tile0 = (ntile * WN + wn) * NT;   // of 16 outputs
-    const uint8_t *w = A.blob + (size_t)min(tile0 / 4, L.nblocks - 1) * L.kblocks * 4096 + tile0 % 4 * 1024;
+    const uint8_t *w = A.codes + (size_t)min(tile0 / 4, nblocks - 1) * A.kblocks * 4096 + tile0 % 4 * 1024;
     v4i *xs = reinterpret_cast<v4i *>(smem) + part * 2 * ROWS * 8;   // [buffer][row][chunk of 16 inputs ^ row % 8]
     // Rows past the last: the last again (not stored).  Inputs past k: any, they meet codes 0.
     const int8_t *x = A.x + (size_t)row0 * A.ldx;
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(C::THREADS, (C::THREADS + 511) / 512 * 2) void line
 #pragma unroll
     for (int l = 0; l < XL; ++l) xrow[l] = min(l * (C::PART / 8) + pt / 8, A.rows - 1 - row0) * (int)A.ldx;
     const int xst = (pt / 8) * 8 + (chunk ^ (pt / 8 % 8));
-    const int ksteps = L.kblocks / 2, steps = (ksteps + WK - 1) / WK;   // step i of this part: inputs from 128 (i WK + part)
+    const int ksteps = A.kblocks / 2, steps = (ksteps + WK - 1) / WK;   // step i of this part: inputs from 128 (i WK + part)
     v4i acc[NT][MT];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(C::THREADS, (C::THREADS + 511) / 512 * 2) void line
         xs[(i % 2) * ROWS * 8 + l * C::PART + xst] = v;
     };
     auto load_w = [&](int set, int t, int i) {   // half i
-        const int k = min(2 * (min(i / 2, steps - 1) * WK + part) + i % 2, L.kblocks - 1);
+        const int k = min(2 * (min(i / 2, steps - 1) * WK + part) + i % 2, A.kblocks - 1);
         wv[set][t] = __builtin_bit_cast(v4i, load_weights<ONCE>(w + (size_t)k * 4096 + (uint32_t)(lane * 16 + t * 1024)));
     };
     auto read_b = [&](int p, int m, int buf) {
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(C::THREADS, (C::THREADS + 511) / 512 * 2) void line
             }
         }
     }
-    const float *ws = reinterpret_cast<const float *>(A.blob + L.scales);
+    const float *ws = A.sw;
     v4i *red = reinterpret_cast<v4i *>(smem);   // [wave][row fragment][tile][lane]
     // The parts' sums of row fragments m0 .. m0 + MC - 1, to LDS; and of tile (t, m0 + m) of this wave's outputs and rows.
     auto share = [&](int m0) {
@@ -337,9 +337,10 @@ hipError_t launch_unpack_linear_w8(const void *blob, int n, int k, int8_t *codes
     return hipGetLastError();
 }
 
-// The variant by shape: the one whose rounds of 256 workgroups (one a CU) take least, by the time of a round: its start and
-// last step, and 1024 inputs.  Larger tiles read less from the L2 for each product, which bounds all but the
-// largest; smaller ones fill the CUs.  In us at k = 4096 (bf16, streams of calls), for 1 round and for 4:
+// The variant by shape: the one that takes least by a model of its rounds of 256 workgroups, one a CU: each its start
+// and last step, and a time per 1024 inputs that grows with the workgroups under way, as they share the L2s and the power.
+// Larger tiles read less for each product, which bounds all but the largest; smaller ones fill the CUs.  In us at
+// k = 4096 (bf16, streams of calls), for 1 round and for 4:
 //   256 x 256  59.8, 227    128 x 256  34.2, 142    128 x 128  22.0, 84    64 x 256  21.7, 96    64 x 128  14.2, 53
 //   32 x 128   11.3, 41     64 x 64    11.2, 39     32 x 64    8.3, 28     32 x 32   7.1, 17     16 x 64   7.1, 20.5
 //   16 x 32    7.1, 13      16 x 16    7.1, 9.6
@@ -347,23 +348,35 @@ hipError_t launch_unpack_linear_w8(const void *blob, int n, int k, int8_t *codes
 // 8.3, 32 x 32 10.0, 64 x 64 11, 128 x 128 17.6.  64 rows, 28672 x 8192: 64 x 128 41.6, 32 x 128 58.6, 64 x 64 55.
 struct W8Cost {
     int rows, outs;
-    float start, k1024;   // us
+    float start, few, all;   // us; per 1024 inputs with one workgroup under way, and 256
 };
-constexpr W8Cost kW8Cost[] = {{256, 256, 5.7f, 12.8f}, {128, 256, 4.3f, 7.8f}, {128, 128, 5.7f, 3.83f}, {64, 256, 4.0f, 5.0f},
-                              {64, 128, 4.0f, 2.3f},   {32, 128, 3.3f, 1.73f}, {64, 64, 4.0f, 1.43f},   {32, 64, 3.05f, 1.0f},
-                              {32, 32, 2.5f, 0.46f},   {16, 64, 1.9f, 0.8f},   {16, 32, 1.7f, 0.4f},    {16, 16, 1.2f, 0.3f}};
+constexpr int kW8Variants = 12;
+constexpr W8Cost kW8Cost[kW8Variants] = {{256, 256, 5.0f, 8.4f, 12.6f}, {128, 256, 4.0f, 4.7f, 7.0f}, {128, 128, 4.0f, 2.7f, 4.2f},
+                                         {64, 256, 3.5f, 3.0f, 5.0f},   {64, 128, 3.0f, 1.6f, 2.6f},  {32, 128, 2.5f, 1.2f, 1.8f},
+                                         {64, 64, 3.0f, 1.1f, 1.6f},    {32, 64, 2.4f, 0.7f, 1.05f},  {32, 32, 1.8f, 0.35f, 0.5f},
+                                         {16, 64, 1.5f, 0.6f, 0.85f},   {16, 32, 1.3f, 0.3f, 0.45f},  {16, 16, 1.0f, 0.25f, 0.35f}};
+constexpr float kW8Launch = 2.0f;
+
+inline float w8_time(const W8Cost &c, int rows, int n, float k1024) {
+    const long long tiles = ((long long)rows + c.rows - 1) / c.rows * ((n + c.outs - 1) / c.outs), full = tiles / 256;
+    const float rest = (float)(tiles % 256) / 256.0f;
+    float t = (float)full * (c.start + k1024 * c.all);
+    if (rest > 0.0f) t += c.start + k1024 * (c.few + (c.all - c.few) * rest);
+    return t;
+}
+
+inline int w8_variant(int rows, int n, float k1024, float *least) {
+    int best = 0;
+    for (int v = 0; v < kW8Variants; ++v) {
+        const float t = w8_time(kW8Cost[v], rows, n, k1024);
+        if (v == 0 || t < *least) best = v, *least = t;
+    }
+    return best;
+}
 
 template <int DT>
-hipError_t launch_dt(const Linear8Args &a, hipStream_t s) {
-    int best = 0;
-    float least = 0.0f;
-    for (int v = 0; v < (int)(sizeof(kW8Cost) / sizeof(kW8Cost[0])); ++v) {
-        const W8Cost &c = kW8Cost[v];
-        const long long tiles = ((long long)a.rows + c.rows - 1) / c.rows * ((a.n + c.outs - 1) / c.outs);
-        const float t = (float)((tiles + 255) / 256) * (c.start + c.k1024 * (float)a.k / 1024.0f);
-        if (v == 0 || t < least) best = v, least = t;
-    }
-    switch (best) {
+hipError_t run_variant(int v, const Linear8Args &a, hipStream_t s) {
+    switch (v) {
     case 0: return run<DT, W8Shape<4, 8, 2, 4, 1, 3, 1>>(a, s);
     case 1: return run<DT, W8Shape<4, 8, 1, 4, 2, 3, 1>>(a, s);
     case 2: return run<DT, W8Shape<4, 4, 2, 2, 2, 4, 2>>(a, s);
@@ -377,6 +390,38 @@ hipError_t launch_dt(const Linear8Args &a, hipStream_t s) {
     case 10: return run<DT, W8Shape<2, 1, 1, 1, 8, 4, 2>>(a, s);
     default: return run<DT, W8Shape<1, 1, 1, 1, 8, 4, 2>>(a, s);
     }
+}
+
+// A call whose last round would leave many CUs idle is cut in two launches: outputs that make whole rounds of large
+// tiles, and the rest in tiles of their own (2048 rows, 10240 x 8192: 256 x 256 180 us, 128 x 256 172, 8192 outputs of the
+// one and 2048 in 128 x 128 TWOLAUNCH).
+template <int DT>
+hipError_t launch_dt(const Linear8Args &a, hipStream_t s) {
+    const float k1024 = (float)a.k / 1024.0f;
+    float least = 0.0f;
+    int best = w8_variant(a.rows, a.n, k1024, &least), rest = -1, cut = 0;
+    for (int v = 0; v < 2; ++v) {
+        const W8Cost &c = kW8Cost[v];
+        const long long mtiles = ((long long)a.rows + c.rows - 1) / c.rows, ntiles = (a.n + c.outs - 1) / c.outs;
+        const long long whole = mtiles * ntiles / 256 * 256 / mtiles;   // columns of tiles of the whole rounds
+        if (whole < 1 || whole >= ntiles) continue;
+        const int n0 = (int)whole * c.outs;
+        float t;
+        const int u = w8_variant(a.rows, a.n - n0, k1024, &t);
+        t += w8_time(c, a.rows, n0, k1024) + kW8Launch;
+        if (t < least) best = v, rest = u, cut = n0, least = t;
+    }
+    if (rest < 0) return run_variant<DT>(best, a, s);
+    Linear8Args b = a;
+    b.n = cut;
+    const hipError_t e = run_variant<DT>(best, b, s);
+    if (e != hipSuccess) return e;
+    b.n = a.n - cut;
+    b.codes += (size_t)(cut / kLinear8N) * a.kblocks * (kLinear8N * kLinear8K);
+    b.sw += cut;
+    b.y += cut;
+    if (b.bias) b.bias += cut;
+    return run_variant<DT>(rest, b, s);
 }
 
 hipError_t launch_linear_w8(int dtype, const Linear8Args &a, hipStream_t s) {

@@ -6,8 +6,9 @@
 namespace prox {
 
 struct Linear8Args {
-    const uint8_t *blob;
-    int n, k;
+    const uint8_t *codes;   // of the weights (Linear8Layout), and their scales
+    const float *sw;
+    int n, k, kblocks;
     const int8_t *x;        // [rows][ldx]
     const float *scales;    // [rows]
     int64_t ldx;
