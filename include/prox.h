@@ -641,7 +641,7 @@ prox_status prox_unpack_linear_w8(const prox_w8_linear *q, int8_t *codes, float 
 /* The projection of rows in 8 bits (d = k; ldc <= PROX_MAX_Q8_PITCH).  codes may hold any int8.
  *   bias  device [n] (2-byte aligned), or NULL
  *   y     device, row b at y + b * ldy, 2-byte aligned; ldy >= n (ignored for one row)
- * One launch, no workspace.  A row's result does not depend on the other rows, nor on
+ * One or two launches, no workspace.  A row's result does not depend on the other rows, nor on
  * their number. */
 prox_status prox_linear_w8(const prox_w8_linear *q, const int8_t *codes, int64_t ldc, const float *scales,
                            int rows, const void *bias, void *y, int64_t ldy, hipStream_t stream);

@@ -916,55 +916,58 @@ def new_rows_q8(rows: int, d: int, device="cuda") -> RowsQ8:
                   torch.empty(rows, dtype=torch.float32, device=device))
 
 
-def _rows16(x: torch.Tensor, what: str):
-    """(rows, d, row stride, C dtype) of 16-bit rows [rows][d], or [d]."""
-    dt = _TORCH_DT.get(x.dtype) if isinstance(x, torch.Tensor) else None
-    if dt is None:
-        raise ValueError(f"{what} must be float16 or bfloat16")
-    shape = x.shape
-    if not 1 <= len(shape) <= 2:
-        raise ValueError(f"{what} must be [rows][d]")
-    rows, ld = _rows2(x, what, x.dtype, shape[-1])
-    return rows, shape[-1], ld, dt
+class _Rows16:
+    """16-bit rows [rows][d], or [d], that a call goes by; its other tensors are compared with them."""
+    __slots__ = ("at", "shape", "strides", "dtype", "index", "code", "rows", "d", "ld")
+
+    def __init__(self, x: torch.Tensor):
+        code = _TORCH_DT.get(x.dtype) if isinstance(x, torch.Tensor) else None
+        if code is None:
+            raise ValueError("x must be float16 or bfloat16")
+        shape = self.shape = x.shape
+        if not 1 <= len(shape) <= 2:
+            raise ValueError("x must be [rows][d]")
+        self.code, self.dtype, self.strides, self.index = code, x.dtype, x.stride(), x.get_device()
+        self.d = shape[-1]
+        self.rows, self.ld = _rows2(x, "x", x.dtype, self.d)
+        self.at = x.data_ptr()
+
+    def like(self, t: torch.Tensor, what: str) -> int:
+        """Row stride of t, which has these rows, type and device."""
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.index:
+            raise ValueError(f"{what} must be a tensor on the device of x")
+        if t.stride() == self.strides and t.shape == self.shape and t.dtype is self.dtype:
+            return self.ld
+        n, ld = _rows2(t, what, self.dtype, self.d)
+        if n != self.rows:
+            raise ValueError(f"{what} must have the rows of x")
+        return ld
+
+    def q8(self, q: RowsQ8):
+        """(row stride, codes, scales) of q, which takes these rows."""
+        n, w, ld, codes, scales, index = q.parts()
+        if n != self.rows or w != self.d or index != self.index:
+            raise ValueError("q must have the shape and the device of x")
+        return ld, codes, scales
 
 
-def _like(t: torch.Tensor, what: str, x: torch.Tensor, rows: int, d: int, ldx: int) -> int:
-    """Row stride of t, which has x's rows, type and device."""
-    if not isinstance(t, torch.Tensor) or t.get_device() != x.get_device():
-        raise ValueError(f"{what} must be a tensor on the device of x")
-    if t.shape == x.shape and t.dtype == x.dtype and t.stride() == x.stride():
-        return ldx
-    n, ld = _rows2(t, what, x.dtype, d)
-    if n != rows:
-        raise ValueError(f"{what} must have the rows of x")
-    return ld
-
-
-def _q8_like(q: RowsQ8, x: torch.Tensor, rows: int, d: int):
-    """(row stride, codes, scales) of q, which takes x's rows."""
-    n, w, ld, codes, scales, index = q.parts()
-    if n != rows or w != d or index != x.get_device():
-        raise ValueError("q must have the shape and the device of x")
-    return ld, codes, scales
-
-
-def _norm(x, rows, d, ldx, dt, y, gain, eps, residual, out, q):
+def _norm(r: _Rows16, device, y, gain, eps, residual, out, q):
     ldy = ldr = ldo = ldc = 0
     py = pr = po = pg = codes = scales = None
     if y is not None:
-        ldy, py = _like(y, "y", x, rows, d, ldx), y.data_ptr()
+        ldy, py = r.like(y, "y"), y.data_ptr()
     if residual is not None:
-        ldr, pr = _like(residual, "residual", x, rows, d, ldx), residual.data_ptr()
+        ldr, pr = r.like(residual, "residual"), residual.data_ptr()
     if out is not None:
-        ldo, po = _like(out, "out", x, rows, d, ldx), out.data_ptr()
+        ldo, po = r.like(out, "out"), out.data_ptr()
     if q is not None:
-        ldc, codes, scales = _q8_like(q, x, rows, d)
+        ldc, codes, scales = r.q8(q)
     if gain is not None:
-        _dev_tensor(gain, "gain", x.dtype)
-        if gain.numel() != d or gain.get_device() != x.get_device():
-            raise ValueError("gain must be [d], on the device of x")
+        if not isinstance(gain, torch.Tensor) or gain.get_device() != r.index or gain.dtype is not r.dtype or \
+                gain.numel() != r.d or not gain.is_contiguous():
+            raise ValueError("gain must be [d], contiguous, of x's type and device")
         pg = gain.data_ptr()
-    _check(_on(x.device, lib().prox_rmsnorm_q8, x.data_ptr(), ldx, py, ldy, pg, rows, d, dt, eps, pr, ldr, po, ldo, codes,
+    _check(_on(device, lib().prox_rmsnorm_q8, r.at, r.ld, py, ldy, pg, r.rows, r.d, r.code, eps, pr, ldr, po, ldo, codes,
                ldc, scales), "prox_rmsnorm_q8")
 
 
@@ -972,10 +975,10 @@ def rmsnorm(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: Optional[to
             residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Root-mean-square norm of the rows r = x + y (x without y), times gain [d], in their own type.  r, rounded to
     that type, goes to `residual` where given; residual or out may be x or y."""
-    rows, d, ldx, dt = _rows16(x, "x")
+    r = _Rows16(x)
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _norm(x, rows, d, ldx, dt, y, gain, eps, residual, out, None)
+    _norm(r, x.device, y, gain, eps, residual, out, None)
     return out
 
 
@@ -983,21 +986,21 @@ def rmsnorm_q8(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: Optional
                residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                q: Optional[RowsQ8] = None) -> RowsQ8:
     """rmsnorm with its result in 8 bits (q, made when not given), and in the rows' own type too where `out` is given."""
-    rows, d, ldx, dt = _rows16(x, "x")
+    r = _Rows16(x)
     if q is None:
-        q = new_rows_q8(rows, d, x.device)
-    _norm(x, rows, d, ldx, dt, y, gain, eps, residual, out, q)
+        q = new_rows_q8(r.rows, r.d, x.device)
+    _norm(r, x.device, y, gain, eps, residual, out, q)
     return q
 
 
 def quant_q8(x: torch.Tensor, up: Optional[torch.Tensor] = None, act: int = SILU, q: Optional[RowsQ8] = None) -> RowsQ8:
     """Rows in 8 bits: of x, or of act(x) * up (SILU or GELU)."""
-    rows, d, ldx, dt = _rows16(x, "x")
-    ldu, pu = (0, None) if up is None else (_like(up, "up", x, rows, d, ldx), up.data_ptr())
+    r = _Rows16(x)
+    ldu, pu = (0, None) if up is None else (r.like(up, "up"), up.data_ptr())
     if q is None:
-        q = new_rows_q8(rows, d, x.device)
-    ldc, codes, scales = _q8_like(q, x, rows, d)
-    _check(_on(x.device, lib().prox_quant_q8, x.data_ptr(), ldx, pu, ldu, _int32(act), rows, d, dt, codes, ldc, scales),
+        q = new_rows_q8(r.rows, r.d, x.device)
+    ldc, codes, scales = r.q8(q)
+    _check(_on(x.device, lib().prox_quant_q8, r.at, r.ld, pu, ldu, _int32(act), r.rows, r.d, r.code, codes, ldc, scales),
            "prox_quant_q8")
     return q
 

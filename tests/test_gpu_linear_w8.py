@@ -280,3 +280,31 @@ def test_a_layer(tokens, dtype):
     R.check_codes(s8.codes, cw)
     R.check_scales(s8.scales, sw)
     check(*lin["down"], s8)
+
+
+# A shape for each kind of tile, and calls that are cut in two launches.
+TILES = [(2717, 2918, 928), (2433, 1563, 917), (1229, 1585, 900), (1425, 1413, 908), (1236, 782, 909), (822, 582, 919), (897, 1025, 905),
+         (618, 390, 903), (305, 385, 1060), (311, 388, 928), (193, 312, 900), (60, 70, 900), (2967, 6729, 902), (2362, 7175, 927),
+         (3104, 5250, 913), (633, 28477, 1112), (347, 23276, 1243), (3334, 2405, 1234), (2476, 3142, 901), (3227, 2314, 902)]
+
+
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("rows,n,k", TILES)
+def test_every_tile(rows, n, k, bias):
+    for more in (0, 130, 260) if bias else (0, 515):       # steps of 128 inputs, in turns of 1 to 3, over up to 8 waves
+        kk = k + more
+        w = prox.pack_linear_w8(randn((n, kk), 1, BF16, 0.02))
+        q, sw = prox.unpack_linear_w8(w)
+        x = rows8(rows, kk, more, pad=16)
+        b = randn((n,), 2, BF16) if bias else None
+        wide = torch.full((rows + 1, n + 5), 7.0, dtype=BF16, device="cuda")
+        y = prox.linear_w8(w, x, bias=b, y=wide[:rows, :n])
+        a = torch.mm(x.codes.double(), q.double().t().contiguous())          # whole numbers below 2^53: exact
+        a = a * sw.double() * x.scales.double()[:, None]
+        want = a if b is None else a + b.double()
+        # three roundings of the product, one of the sum, half a step of the type
+        room = 3.01 * 2.0 ** -24 * a.abs() + 2.0 ** -24 * want.abs()
+        room = room + 2.0 ** -8 * (want.abs() + room) + 2.0 ** -134
+        far = (y.double() - want).abs()
+        assert (far <= room).all(), f"{rows}x{n}x{kk}: {(far / room).max().item()}"
+        assert (wide[rows] == 7).all() and (wide[:, n:] == 7).all()
