@@ -141,12 +141,13 @@ __device__ __forceinline__ V wave_join(V v, F f) {   // f symmetric: the same bi
     return f(a, b);
 }
 
-// A value joined over the T threads of a row, the same in each of them.  T = 64: a wave by itself.
-template <int T, typename V, typename F>
+// A value joined over the T threads of a row, the same in each of them.  T = 64: a wave by itself.  AGAIN: lds has
+// been used before.
+template <int T, bool AGAIN, typename V, typename F>
 __device__ __forceinline__ V row_join(V v, V *lds, F f) {
     v = wave_join(v, f);
     if constexpr (T > 64) {
-        __syncthreads();   // an earlier use of lds is over
+        if constexpr (AGAIN) __syncthreads();
         if (lane_id() == 0) lds[threadIdx.x / kWave] = v;
         __syncthreads();
         v = lds[0];
@@ -154,6 +155,19 @@ __device__ __forceinline__ V row_join(V v, V *lds, F f) {
         for (int w = 1; w < T / 64; ++w) v = f(v, lds[w]);
     }
     return v;
+}
+// Two of them behind one barrier.
+template <int T, typename V, typename F, typename W, typename G>
+__device__ __forceinline__ void row_join2(V &v, V *lds, F f, W &u, W *lds2, G g) {
+    v = wave_join(v, f);
+    u = wave_join(u, g);
+    if constexpr (T > 64) {
+        if (lane_id() == 0) lds[threadIdx.x / kWave] = v, lds2[threadIdx.x / kWave] = u;
+        __syncthreads();
+        v = lds[0], u = lds2[0];
+#pragma unroll
+        for (int w = 1; w < T / 64; ++w) v = f(v, lds[w]), u = g(u, lds2[w]);
+    }
 }
 struct Add {
     __device__ __forceinline__ double operator()(double a, double b) const { return a + b; }
@@ -254,8 +268,7 @@ __global__ __launch_bounds__(C::threads) void rmsnorm_kernel(NormArgs A) {
             top = max(top, __float_as_uint(v * elem<DT>(g[c], e)) & 0x7FFFFFFFu);   // NaN above all
         }
     });
-    sum = row_join<T>(sum, sums, Add());
-    top = row_join<T>(top, tops, Most());
+    row_join2<T>(sum, sums, Add(), top, tops, Most());
     const double mean = fma(sum, A.inv_d, (double)A.eps);
     const float topf = __uint_as_float(top);
     // Products and 1 / rms well inside 32 bits, everything finite.
@@ -299,8 +312,8 @@ __global__ __launch_bounds__(C::threads) void rmsnorm_kernel(NormArgs A) {
             most = fmax(most, fabs(p));
         }
     });
-    most = row_join<T>(most, sums, Most());
-    bad = row_join<T>(bad, sums, Most());
+    most = row_join<T, true>(most, sums, Most());
+    bad = row_join<T, true>(bad, sums, Most());
     const bool finite = bad == 0.0 && sum < INFINITY;
     if (t == 0 && A.codes) A.scales[row] = finite ? (float)(most * inv / 127.0) : quiet_nan();
     each<CH>([&](auto c) {
@@ -382,7 +395,7 @@ __global__ __launch_bounds__(C::threads) void quant_kernel(QuantArgs A) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(elem<DT>(v[c], e)) & 0x7FFFFFFFu);   // NaN above all
     });
-    top = row_join<T>(top, tops, Most());
+    top = row_join<T, false>(top, tops, Most());
     const float topf = __uint_as_float(top), s = 127.0f / topf;
     const bool finite = top < 0x7F800000u, plain = topf >= 0x1p-100f;   // s is a finite number
     if (t == 0) A.scales[row] = finite ? (float)((double)topf * (1.0 / 127.0)) : quiet_nan();
@@ -413,7 +426,7 @@ __global__ __launch_bounds__(C::threads) void quant_kernel(QuantArgs A) {
 // worked out when the row's registers are free, from the inputs again.
 constexpr int kListed = 256;
 struct GatedRow {
-    uint32_t n_top, n_near, top, least;
+    uint32_t n_top, n_near;
     uint16_t may_top[kListed], near[kListed];   // elements of the row
 };
 
@@ -421,7 +434,7 @@ template <int DT, class C, bool TAIL, int ACT>
 __global__ __launch_bounds__(C::threads) void gated_kernel(QuantArgs A) {
     constexpr bool WAVE = C::wave;
     constexpr int T = C::T, CH = C::CH;
-    __shared__ uint32_t parts[T / 64];
+    __shared__ uint32_t parts[T / 64], parts2[T / 64];
     __shared__ GatedRow lists[WAVE ? 4 : 1];
     const int row = WAVE ? (int)blockIdx.x * 4 + (int)threadIdx.x / 64 : (int)blockIdx.x;
     const int t = WAVE ? lane_id() : (int)threadIdx.x;
@@ -457,9 +470,9 @@ __global__ __launch_bounds__(C::threads) void gated_kernel(QuantArgs A) {
         });
     }
     const float mine = __uint_as_float(top);
-    top = row_join<T>(top, parts, Most());
-    // Of gates below 0, bits order like sizes.
-    low = __uint_as_float(row_join<T>(__float_as_uint(low) & 0x7FFFFFFFu, parts, Most()) | 0x80000000u);
+    uint32_t lows = __float_as_uint(low) & 0x7FFFFFFFu;   // of gates below 0, bits order like sizes
+    row_join2<T>(top, parts, Most(), lows, parts2, Most());
+    low = __uint_as_float(lows | 0x80000000u);
     const float topf = __uint_as_float(top);
     bool slow = !(topf >= 0x1p-60f && topf <= 0x1p100f);   // ends of the range, not finite
     if (!slow) {
@@ -495,7 +508,7 @@ __global__ __launch_bounds__(C::threads) void gated_kernel(QuantArgs A) {
         uint32_t most = 0;
 #pragma unroll 1
         for (int i = t; i < n; i += T) most = max(most, __float_as_uint(exact(slow ? i : (int)L.may_top[i])) & 0x7FFFFFFFu);
-        return row_join<T>(most, parts, Most());
+        return row_join<T, true>(most, parts, Most());
     };
     uint32_t most = largest();
     if (!slow && __uint_as_float(most) > topf * (1.0f + 0x1p-13f)) {   // a gate below kFarGate made it: the codes are not near

@@ -924,13 +924,19 @@ class _Rows16:
         code = _TORCH_DT.get(x.dtype) if isinstance(x, torch.Tensor) else None
         if code is None:
             raise ValueError("x must be float16 or bfloat16")
-        shape = self.shape = x.shape
-        if not 1 <= len(shape) <= 2:
+        shape, strides, index = x.shape, x.stride(), x.get_device()
+        if not x.is_cuda:
+            raise ValueError("x must be a CUDA (HIP) tensor")
+        if len(shape) == 2:
+            rows, d = shape
+        elif len(shape) == 1:
+            rows, d = 1, shape[0]
+        else:
             raise ValueError("x must be [rows][d]")
-        self.code, self.dtype, self.strides, self.index = code, x.dtype, x.stride(), x.get_device()
-        self.d = shape[-1]
-        self.rows, self.ld = _rows2(x, "x", x.dtype, self.d)
-        self.at = x.data_ptr()
+        if d > 1 and strides[-1] != 1:
+            raise ValueError("x must be [rows][d] with contiguous rows")
+        self.shape, self.strides, self.index, self.code, self.dtype = shape, strides, index, code, x.dtype
+        self.rows, self.d, self.ld, self.at = rows, d, d if rows == 1 else strides[0], x.data_ptr()
 
     def like(self, t: torch.Tensor, what: str) -> int:
         """Row stride of t, which has these rows, type and device."""
