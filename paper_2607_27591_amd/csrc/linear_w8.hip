@@ -1,8 +1,8 @@
 // Projections on 8-bit integers, y = (c_x c_w^T) sigma_x sigma_w (+ bias): weights packed and unpacked, and
 // the product: y^T = W x^T as 16 x 16 x 64 MFMAs, exact in 32 bits.  The weights go from the caches to registers as
 // operands (every wave's outputs are its own, and their layout is the operands'), x through LDS, where the waves share it;
-// the sums are scaled and rounded once.  Few rows are bound by the weights' bytes (28672 x 8192, 16 rows 38.4 us,
-// 6.1 TB/s), many by power: at 4096 rows the clock falls to 1.8 GHz (715 us, 2690 TOP/s).  What saves power there:
+// the sums are scaled and rounded once.  Few rows are bound by the weights' bytes (28672 x 8192, 16 rows 40.1 us,
+// 5.9 TB/s), many by power: at 4096 rows the clock falls to 1.8 GHz (719 us, 2675 TOP/s).  What saves power there:
 // 16 x 16 x 64 products rather than 32 x 32 x 32 (random operands, nothing else: 3695 and 3160 TOP/s), one operand
 // kept from product to product (4075 TOP/s).
 #include "linear_w8.hpp"
@@ -95,7 +95,7 @@ __device__ __forceinline__ uint32_t to_pair(float a, float b) {
     else return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
 }
 
-// Weights that are read once by a call (ONCE) are loaded as a stream: 28672 x 8192, 16 rows 38.4 us, without 44.6.
+// Weights that are read once by a call (ONCE) are loaded as a stream: 28672 x 8192, 16 rows 40.1 us, without 44.6.
 template <bool ONCE>
 __device__ __forceinline__ u32x4 load_weights(const uint8_t *p) {
     if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));

@@ -459,6 +459,11 @@ __global__ __launch_bounds__(C::threads) void gated_kernel(QuantArgs A) {
         });
         each<CH>([&](auto c) {
             least[c] = 0.0f;
+            if (c > 0 && c * T * 8 >= d) {   // no thread has any
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[c][e] = 0.0f;
+                return;
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float g = elem<DT>(gv[c], e);
