@@ -56,6 +56,13 @@ __device__ __forceinline__ uint16_t float_to_half(float v) {
     else return float_to_f16_rne(v);
 }
 
+// Two values rounded to the dtype (NaN stays NaN).
+template <int DT>
+__device__ __forceinline__ uint32_t round_pair(float a, float b) {
+    if constexpr (DT == kBF16) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+    else return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+}
+
 // Two-term dot product with fp32 accumulation: a.lo*b.lo + a.hi*b.hi + c.
 template <int DT>
 __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {

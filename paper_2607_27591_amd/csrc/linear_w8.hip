@@ -11,12 +11,6 @@ namespace prox {
 
 namespace {
 
-template <int DT>
-__device__ __forceinline__ uint16_t to_half(float v) {   // NaN stays NaN
-    if constexpr (DT == kBF16) return __builtin_bit_cast(uint16_t, (__bf16)v);
-    else return float_to_f16_rne(v);
-}
-
 // Packing: a workgroup takes the 16 outputs of a tile, 16 lanes each, 16 inputs a lane and step, and reads them twice
 // (the second time from the L2), so that it writes whole runs of 1024 bytes.  28672 x 8192 270 us (705 MB, 2.6 TB/s).
 // A code is the exact quotient's, as rows in 8 bits have it: where 32 bits leave it near the middle of two, 64 decide.
@@ -88,13 +82,6 @@ __global__ __launch_bounds__(256) void unpack_w8_kernel(const uint8_t *__restric
     }
 }
 
-// Two values rounded to the dtype (NaN stays NaN).
-template <int DT>
-__device__ __forceinline__ uint32_t to_pair(float a, float b) {
-    if constexpr (DT == kBF16) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
-    else return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
-}
-
 // Weights that are read once by a call (ONCE) are loaded as a stream: 28672 x 8192, 16 rows 40.1 us, without 44.6.
 template <bool ONCE>
 __device__ __forceinline__ u32x4 load_weights(const uint8_t *p) {
@@ -109,7 +96,7 @@ __device__ __forceinline__ uint2 finish4(const Linear8Args &A, const float *ws, 
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = fmaf((float)acc[e] * sw[e], sx, A.bias ? half_to_float<DT>(A.bias[min(j + e, A.n - 1)]) : 0.0f);
-    return make_uint2(to_pair<DT>(v[0], v[1]), to_pair<DT>(v[2], v[3]));
+    return make_uint2(round_pair<DT>(v[0], v[1]), round_pair<DT>(v[2], v[3]));
 }
 
 // W8Shape: a wave takes 16 NT outputs by 16 MT rows; a workgroup WN x WM waves, WK times: its WK parts take a step of

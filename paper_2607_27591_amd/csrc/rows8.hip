@@ -87,13 +87,6 @@ __device__ __forceinline__ void set_code(uint2 &v, int e, uint32_t code) {
     else v.y = (v.y & ~m) | k;
 }
 
-// Two values rounded to the dtype (NaN stays NaN).
-template <int DT>
-__device__ __forceinline__ uint32_t round_pair(float a, float b) {
-    if constexpr (DT == kBF16) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
-    else return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
-}
-
 // Moves on the VALU, lane ^ 1, 2 and, among 16 and 64 lanes, rotations that pair the halves.
 template <int STEP>
 __device__ __forceinline__ uint32_t peer(uint32_t v) {

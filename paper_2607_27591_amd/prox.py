@@ -973,7 +973,7 @@ def _norm(r: _Rows16, device, y, gain, eps, residual, out, q):
                 gain.numel() != r.d or not gain.is_contiguous():
             raise ValueError("gain must be [d], contiguous, of x's type and device")
         pg = gain.data_ptr()
-    _check(_on(device, lib().prox_rmsnorm_q8, r.at, r.ld, py, ldy, pg, r.rows, r.d, r.code, eps, pr, ldr, po, ldo, codes,
+    _check(_on(device, lib().prox_rmsnorm_q8, r.at, r.ld, py, ldy, pg, r.rows, r.d, r.code, float(eps), pr, ldr, po, ldo, codes,
                ldc, scales), "prox_rmsnorm_q8")
 
 

@@ -31,7 +31,7 @@ def norm(x, y, gain, eps, dtype):
     with np.errstate(all="ignore"):
         r = x if y is None else to_type(x + y, dtype)
         p = r if gain is None else r * gain
-        mean = (r * r).mean(-1) + eps
+        mean = (r * r).mean(-1) + float(np.float32(eps))
         inv = np.where(mean > 0, 1 / np.sqrt(mean), 0.0)
         n = p * inv[:, None]
     fine = np.isfinite(r).all(-1)

@@ -328,3 +328,47 @@ def test_offsets_past_32_bits():
     assert torch.equal(q.codes, want.codes) and torch.equal(prox.read_q8(q), prox.read_q8(want))
     out = torch.empty_strided((rows, d), (pitch, 1), dtype=BF16, device="cuda")
     assert torch.equal(prox.rmsnorm(x, x, out=out), prox.rmsnorm(x.contiguous(), x.contiguous()))
+
+
+def test_numbers_of_other_kinds():
+    x = hidden(3, 200, 1, BF16)
+    want = prox.rmsnorm(x, eps=1.0)
+    assert torch.equal(prox.rmsnorm(x, eps=1), want) and torch.equal(prox.rmsnorm(x, eps=np.float32(1)), want)
+    assert torch.equal(prox.rmsnorm(x, eps=torch.tensor(1.0)), want)
+    with pytest.raises(TypeError):
+        prox.quant_q8(x, x, act=0.5)
+
+
+def test_many_short_rows():
+    # More rows than the chip has waves, of one element and of odd widths.
+    for rows, d in ((100003, 1), (70001, 9), (50000, 65)):
+        x, u = randn((rows, d), d, F16), randn((rows, d), d + 1, F16)
+        check_quant(x, None, 0, f"{rows}x{d}")
+        check_quant(x, u, prox.SILU, f"{rows}x{d}")
+        check_norm(x, u, None, 1e-6, f"{rows}x{d}")
+
+
+@pytest.mark.parametrize("act", [prox.SILU, prox.GELU])
+def test_every_element_may_be_the_largest(act):
+    # Rows of one value, and of two next to each other: more of them than a list holds.
+    for d in (100, 300, 3000, 20000):
+        g = torch.full((4, d), 1.25, dtype=BF16, device="cuda")
+        u = torch.full((4, d), -0.75, dtype=BF16, device="cuda")
+        u[1, ::2] = -0.7539
+        u[2, ::3] *= 0.5                      # codes of 63.5: a tie
+        g[3, 5:] = -100.0                     # far gates with one near
+        check_quant(g, u, act, f"{d}")
+        g[3] = -100.0
+        u[3] = torch.linspace(1, 3e38, d).to(BF16)
+        check_quant(g, u, act, f"{d}, far gates")
+
+
+@pytest.mark.parametrize("act", [prox.SILU, prox.GELU])
+def test_a_far_gate_makes_the_largest(act):
+    # A gate far below 0 whose activation, of a huge up, exceeds the others'.
+    for d in (64, 1000, 9000):
+        g, u = randn((3, d), 1, BF16), randn((3, d), 2, BF16)
+        far = -85.0 if act == prox.SILU else -12.5
+        g[:, d // 3] = far
+        u[0, d // 3], u[1, d // 3], u[2, d // 3] = 3e37, 1e34, -3.3e38
+        check_quant(g, u, act, f"{d}")
