@@ -339,8 +339,9 @@ __device__ __forceinline__ float exact_act(float g, float u) {
 // The same in 32 bits, for gates from kFarGate on; off by rel_act(g) of its size at most, g the least of some gates and 0:
 //   SiLU: the exponent's product rounds (1.5 |g| 2^-24 of the exponential, which matters where g < 0), exp2 and 1 / x are
 //   good to 2^-23, three more roundings: (1.5 |g| + 8) 2^-24;
-//   GELU: Phi(-|z|) = exp(-z^2 / 2) t Q(t), t = 1 / (1 + |z| / 4), with a polynomial fitted to exp(z^2 / 2) Phi(-z)
-//   over [0, 13] (off by 4.7e-8 of it); the exponent rounds like z^2: (1.5 g^2 + 16) 2^-24.
+//   GELU: z Phi(z) = max(z, 0) - |z| Phi(-|z|), Phi(-z) = exp(-z^2 / 2) t Q(t), t = 1 / (1 + 0.305 z), with a
+//   polynomial of degree 7 fitted to exp(z^2 / 2) Phi(-z) over [0, 13] (off by 9.6e-8 of it); the exponent rounds like
+//   z^2: (1.5 g^2 + 16) 2^-24.
 template <int ACT>
 constexpr float kFarGate = ACT == kActSilu ? -80.0f : -12.0f;
 template <int ACT>
@@ -348,18 +349,17 @@ __device__ __forceinline__ float fast_act(float g, float u) {
     if constexpr (ACT == kActSilu) {
         return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f)) * u;
     } else {
-        const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.25f, 1.0f));
-        float q = 0.026892656f;
-        q = fmaf(q, t, -0.15860404f);
-        q = fmaf(q, t, 0.30836424f);
-        q = fmaf(q, t, -0.22015412f);
-        q = fmaf(q, t, 0.21198905f);
-        q = fmaf(q, t, 0.028413807f);
-        q = fmaf(q, t, 0.104949996f);
-        q = fmaf(q, t, 0.09833994f);
-        q = fmaf(q, t, 0.09980845f);
-        const float h = q * t * __builtin_amdgcn_exp2f(g * g * -0.72134752f);
-        return g * (g < 0.0f ? h : 1.0f - h) * u;
+        const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.305f, 1.0f));
+        float q = 0.036698908f;
+        q = fmaf(q, t, -0.15298693f);
+        q = fmaf(q, t, 0.18571411f);
+        q = fmaf(q, t, -0.03797383f);
+        q = fmaf(q, t, 0.12101983f);
+        q = fmaf(q, t, 0.10342152f);
+        q = fmaf(q, t, 0.1224667f);
+        q = fmaf(q, t, 0.12163974f);
+        const float h = q * t * __builtin_amdgcn_exp2f(g * g * -0.72134752f);   // Phi(-|g|)
+        return fmaf(-fabsf(g), h, fmaxf(g, 0.0f)) * u;
     }
 }
 template <int ACT>
