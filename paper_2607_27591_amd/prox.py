@@ -886,6 +886,17 @@ def kv_attn(c: KVCache, s: KVSeqs, q: torch.Tensor, scale: Optional[float] = Non
 # Rows and weights in 8 bits
 # ---------------------------------------------------------------------------
 
+def _enqueue(index: int, f, args: tuple, where: str) -> None:
+    """f(*args, stream) on the current stream of device `index`, which may not be the current device."""
+    if index != _current_device() or _raw_stream is None:
+        with torch.cuda.device(index):
+            status = f(*args, torch.cuda.current_stream(index).cuda_stream)
+    else:
+        status = f(*args, _raw_stream(index))
+    if status:
+        raise ProxError(status, where)
+
+
 @dataclasses.dataclass(frozen=True)
 class RowsQ8(_Handle):
     """Rows in 8 bits: device codes int8 [rows][d], whose rows stand a multiple of 16 bytes apart, and scales
@@ -957,7 +968,7 @@ class _Rows16:
         return ld, codes, scales
 
 
-def _norm(r: _Rows16, device, y, gain, eps, residual, out, q):
+def _norm(r: _Rows16, y, gain, eps, residual, out, q):
     ldy = ldr = ldo = ldc = 0
     py = pr = po = pg = codes = scales = None
     if y is not None:
@@ -973,8 +984,8 @@ def _norm(r: _Rows16, device, y, gain, eps, residual, out, q):
                 gain.numel() != r.d or not gain.is_contiguous():
             raise ValueError("gain must be [d], contiguous, of x's type and device")
         pg = gain.data_ptr()
-    _check(_on(device, lib().prox_rmsnorm_q8, r.at, r.ld, py, ldy, pg, r.rows, r.d, r.code, float(eps), pr, ldr, po, ldo, codes,
-               ldc, scales), "prox_rmsnorm_q8")
+    _enqueue(r.index, lib().prox_rmsnorm_q8, (r.at, r.ld, py, ldy, pg, r.rows, r.d, r.code, float(eps), pr, ldr, po, ldo, codes,
+                                              ldc, scales), "prox_rmsnorm_q8")
 
 
 def rmsnorm(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -984,7 +995,7 @@ def rmsnorm(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: Optional[to
     r = _Rows16(x)
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _norm(r, x.device, y, gain, eps, residual, out, None)
+    _norm(r, y, gain, eps, residual, out, None)
     return out
 
 
@@ -995,7 +1006,7 @@ def rmsnorm_q8(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: Optional
     r = _Rows16(x)
     if q is None:
         q = new_rows_q8(r.rows, r.d, x.device)
-    _norm(r, x.device, y, gain, eps, residual, out, q)
+    _norm(r, y, gain, eps, residual, out, q)
     return q
 
 
@@ -1006,8 +1017,7 @@ def quant_q8(x: torch.Tensor, up: Optional[torch.Tensor] = None, act: int = SILU
     if q is None:
         q = new_rows_q8(r.rows, r.d, x.device)
     ldc, codes, scales = r.q8(q)
-    _check(_on(x.device, lib().prox_quant_q8, r.at, r.ld, pu, ldu, _int32(act), r.rows, r.d, r.code, codes, ldc, scales),
-           "prox_quant_q8")
+    _enqueue(r.index, lib().prox_quant_q8, (r.at, r.ld, pu, ldu, _int32(act), r.rows, r.d, r.code, codes, ldc, scales), "prox_quant_q8")
     return q
 
 
@@ -1019,7 +1029,7 @@ def read_q8(q: RowsQ8, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     _dev_tensor(out, "out", torch.float32)
     if out.shape != q.codes.shape or out.get_device() != index:
         raise ValueError("out must be [rows][d], on the device of q")
-    _check(_on(out.device, lib().prox_read_q8, codes, ldc, scales, rows, d, out.data_ptr()), "prox_read_q8")
+    _enqueue(index, lib().prox_read_q8, (codes, ldc, scales, rows, d, out.data_ptr()), "prox_read_q8")
     return out
 
 
@@ -1086,7 +1096,7 @@ def linear_w8(w: LinearW8, x: RowsQ8, bias: Optional[torch.Tensor] = None, y: Op
         pb = bias.data_ptr()
     if y.get_device() != index or w.blob.get_device() != index:
         raise ValueError("every tensor of a call must be on one device")
-    _check(_on(y.device, lib().prox_linear_w8, w.pointer(), codes, ldc, scales, rows, pb, y.data_ptr(), ldy), "prox_linear_w8")
+    _enqueue(index, lib().prox_linear_w8, (w.pointer(), codes, ldc, scales, rows, pb, y.data_ptr(), ldy), "prox_linear_w8")
     return y
 
 
