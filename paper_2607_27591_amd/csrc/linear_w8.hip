@@ -231,13 +231,16 @@ __global__ __launch_bounds__(C::THREADS, (C::THREADS + 511) / 512 * 2) void line
     }
     const float *ws = A.sw;
     v4i *red = reinterpret_cast<v4i *>(smem);   // [wave][row fragment][tile][lane]
-    // The parts' sums of row fragments m0 .. m0 + MC - 1, to LDS; and of tile (t, m0 + m) of this wave's outputs and rows.
+    // The parts' sums of row fragments m0 .. m0 + MC - 1, to LDS (but those that the part itself adds up, if it takes
+    // whole fragments); and of tile (t, m0 + m) of this wave's outputs and rows.
     auto share = [&](int m0) {
         __syncthreads();
 #pragma unroll
-        for (int m = 0; m < C::MC; ++m)
+        for (int m = 0; m < C::MC; ++m) {
+            if (C::TILE && m / C::MINE == part) continue;
 #pragma unroll
             for (int t = 0; t < NT; ++t) red[((wave * C::MC + m) * NT + t) * kWave + lane] = acc[t][m0 + m];
+        }
         __syncthreads();
     };
     auto sum = [&](int t, int m) {
@@ -259,7 +262,17 @@ __global__ __launch_bounds__(C::THREADS, (C::THREADS + 511) / 512 * 2) void line
 #pragma unroll
             for (int f = 0; f < MINE; ++f)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) v[t][f] = WK > 1 ? sum(t, part * MINE + f) : acc[t][m0 + f];
+                for (int t = 0; t < 4; ++t) {
+                    if constexpr (WK == 1) {
+                        v[t][f] = acc[t][m0 + f];
+                    } else {
+                        v[t][f] = v4i{0, 0, 0, 0};
+#pragma unroll
+                        for (int g = 0; g < WK; ++g)
+                            v[t][f] += g == part ? acc[t][m0 + g * MINE + f]
+                                                 : red[(((g * WM * WN + wave % (WM * WN)) * C::MC + part * MINE + f) * NT + t) * kWave + lane];
+                    }
+                }
             if constexpr (WK > 1) __syncthreads();
             else wave_lds_fence();
             if (j0 >= A.n) continue;
