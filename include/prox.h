@@ -592,7 +592,7 @@ prox_status prox_kv_attn(const prox_kv_cache *c, const prox_kv_seqs *s, const vo
  *   r = x + y  rounded to the dtype (y NULL: r = x),
  *   p_i = r_i gain_i (gain NULL: 1),  n = p / sqrt(mean(r^2) + eps).
  *   r       or NULL: where r goes
- *   out     or NULL: n rounded to the dtype (as fp32 of 64-bit sums)
+ *   out     or NULL: n rounded to the dtype (computed in fp32, the sum of squares in 64 bits)
  *   codes, scales  or both NULL: n in 8 bits; sigma = fp32(A / (127 sqrt(mean(r^2) + eps)))
  * One of out and codes at least.  r or out may be x or y, with their stride; other
  * overlaps are not allowed.  gain: device [d].  eps >= 0, finite; a row of zeros gives zeros for
