@@ -2,7 +2,7 @@
 // the product: y^T = W x^T as 16 x 16 x 64 MFMAs, exact in 32 bits.  The weights go from the caches to registers as
 // operands (every wave's outputs are its own, and their layout is the operands'), x through LDS, where the waves share it;
 // the sums are scaled and rounded once.  Few rows are bound by the weights' bytes (28672 x 8192, 16 rows 40.1 us,
-// 5.9 TB/s), many by power: at 4096 rows the clock falls to 1.8 GHz (719 us, 2675 TOP/s).  What saves power there:
+// 5.9 TB/s), many by power: at 4096 rows the clock falls to 1.85 GHz (697 to 711 us, 2710 to 2760 TOP/s).  What saves power there:
 // 16 x 16 x 64 products rather than 32 x 32 x 32 (random operands, nothing else: 3695 and 3160 TOP/s), one operand
 // kept from product to product (4075 TOP/s).
 #include "linear_w8.hpp"
