@@ -897,6 +897,12 @@ def _enqueue(index: int, f, args: tuple, where: str) -> None:
         raise ProxError(status, where)
 
 
+def _check_sizes(rows: int, d: int) -> None:
+    """Refuses what a C int would lose the upper bits of; the library's own limits lie far below."""
+    if rows >= 2 ** 31 or d >= 2 ** 31:
+        raise ProxError(2, "rows in 8 bits")
+
+
 @dataclasses.dataclass(frozen=True)
 class RowsQ8(_Handle):
     """Rows in 8 bits: device codes int8 [rows][d], whose rows stand a multiple of 16 bytes apart, and scales
@@ -912,6 +918,7 @@ class RowsQ8(_Handle):
             if c.dim() != 2:
                 raise ValueError("codes must be [rows][d]")
             rows, ld = _rows2(c, "codes", torch.int8, c.shape[1])
+            _check_sizes(rows, c.shape[1])
             _dev_tensor(s, "scales", torch.float32)
             if tuple(s.shape) != (rows,):
                 raise ValueError("scales must be [rows]")
@@ -946,6 +953,7 @@ class _Rows16:
             raise ValueError("x must be [rows][d]")
         if d > 1 and strides[-1] != 1:
             raise ValueError("x must be [rows][d] with contiguous rows")
+        _check_sizes(rows, d)
         self.shape, self.strides, self.index, self.code, self.dtype = shape, strides, index, code, x.dtype
         self.rows, self.d, self.ld, self.at = rows, d, d if rows == 1 else strides[0], x.data_ptr()
 

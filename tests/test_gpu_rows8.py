@@ -291,6 +291,22 @@ def test_refusals_on_the_device():
         prox.read_q8(prox.RowsQ8(torch.zeros((4, 65), dtype=torch.int8, device="cuda"), q.scales))   # rows 65 bytes apart
 
 
+@pytest.mark.parametrize("shape", [(2 ** 32 + 1, 1), (2 ** 31, 1), (1, 2 ** 32 + 1)], ids=str)
+def test_sizes_past_32_bits_are_refused(shape):
+    """They do not lose their upper bits, and one row or value is not taken for all."""
+    x = randn((1, 1), 1, BF16)
+    x = x.expand(shape) if shape[1] == 1 else torch.empty(shape, dtype=BF16, device="cuda")
+    for call in (lambda: prox.rmsnorm(x, out=x), lambda: prox.quant_q8(x, x)):
+        with pytest.raises(prox.ProxError) as e:
+            call()
+        assert e.value.status == 2
+    codes = torch.zeros((1, 1), dtype=torch.int8, device="cuda")
+    codes = codes.expand(shape) if shape[1] == 1 else torch.empty(shape, dtype=torch.int8, device="cuda")
+    with pytest.raises(prox.ProxError) as e:
+        prox.read_q8(prox.RowsQ8(codes, torch.zeros(1, device="cuda")), out=torch.zeros((1, 1), device="cuda"))
+    assert e.value.status == 2
+
+
 @pytest.mark.parametrize("d", [300, 1500, 9000])
 def test_capture_and_streams(d):
     x, y, gain, up = (randn((40, d), i, BF16) for i in (1, 2, 3, 4))
