@@ -913,7 +913,7 @@ class RowsQ8(_Handle):
     def parts(self):
         """(rows, d, row stride, codes, scales, device index), as a call takes them."""
         kept, c, s = self._kept, self.codes, self.scales
-        key = (c.data_ptr(), s.data_ptr(), c.shape)
+        key = (c.data_ptr(), s.data_ptr(), c.shape, c.stride(), s.numel(), s.is_contiguous())
         if kept is None or kept[0] != key:
             if c.dim() != 2:
                 raise ValueError("codes must be [rows][d]")

@@ -307,6 +307,22 @@ def test_sizes_past_32_bits_are_refused(shape):
     assert e.value.status == 2
 
 
+def test_rows_that_are_laid_out_anew():
+    """Codes and scales whose shape or strides change in place between two calls on one RowsQ8."""
+    x = randn((16, 64), 2, BF16)
+    want = prox.quant_q8(x)
+    q = prox.RowsQ8(torch.zeros(16 * 96, dtype=torch.int8, device="cuda").as_strided((16, 64), (80, 1)), torch.zeros(16, device="cuda"))
+    for pitch in (80, 96, 64):
+        q.codes.as_strided_((16, 64), (pitch, 1))
+        prox.quant_q8(x, q=q)
+        assert torch.equal(q.codes, want.codes) and torch.equal(prox.read_q8(q), prox.read_q8(want)), pitch
+    q.scales.as_strided_((8,), (2,))
+    with pytest.raises(ValueError):
+        prox.read_q8(q)
+    q.scales.as_strided_((16,), (1,))
+    prox.read_q8(q)
+
+
 @pytest.mark.parametrize("d", [300, 1500, 9000])
 def test_capture_and_streams(d):
     x, y, gain, up = (randn((40, d), i, BF16) for i in (1, 2, 3, 4))
