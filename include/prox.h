@@ -19,7 +19,7 @@
  *  - Calls are reentrant when they use distinct workspaces.  Two calls that
  *    share a workspace must be ordered on one stream.
  *  - 16-bit tensors are IEEE fp16 or bf16 bit patterns (prox_dtype).  Inputs
- *    must be finite.
+ *    must be finite, but where an entry point says what comes of others.
  */
 #ifndef PROX_H
 #define PROX_H
@@ -596,7 +596,9 @@ prox_status prox_kv_attn(const prox_kv_cache *c, const prox_kv_seqs *s, const vo
  *   codes, scales  or both NULL: n in 8 bits; sigma = fp32(A / (127 sqrt(mean(r^2) + eps)))
  * One of out and codes at least.  r or out may be x or y, with their stride; other
  * overlaps are not allowed.  gain: device [d].  eps >= 0, finite; a row of zeros gives zeros for
- * any.  One launch, no workspace.  prox_add_rmsnorm differs: its r is not rounded, and has no gain.
+ * any.  Rows that are not finite follow the formula in r and out: a NaN in r makes all of its row NaN, an
+ * infinite r its own n NaN and the others 0.  One launch, no workspace.  prox_add_rmsnorm differs: its r is
+ * not rounded, and has no gain.
  */
 prox_status prox_rmsnorm_q8(const void *x, int64_t ldx, const void *y, int64_t ldy, const void *gain, int rows,
                             int d, prox_dtype dtype, float eps, void *r, int64_t ldr, void *out, int64_t ldo,

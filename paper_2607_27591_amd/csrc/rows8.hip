@@ -295,7 +295,7 @@ __global__ __launch_bounds__(C::threads) void rmsnorm_kernel(NormArgs A) {
         return;
     }
     // Rows at the ends of the range or not finite, in 64 bits.
-    const double inv = mean > 0.0 ? 1.0 / sqrt(mean) : 0.0;   // a row of zeros and eps 0: zeros
+    const double inv = mean == 0.0 ? 0.0 : 1.0 / sqrt(mean);   // a row of zeros and eps 0: zeros; a NaN spoils its row
     double most = 0.0, bad = 0.0;
     each<CH>([&](auto c) {
 #pragma unroll 1

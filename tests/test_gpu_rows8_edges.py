@@ -1,0 +1,67 @@
+"""Rows in 8 bits where a value of the row decides about the others: against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import rows8_ref as R
+from layer_ref import f64
+from paper_2607_27591_amd import prox
+
+pytestmark = pytest.mark.gpu
+BF16, F16 = torch.bfloat16, torch.float16
+
+
+def randn(shape, seed, dtype, scale=1.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * scale).to(dtype).cuda()
+
+
+def norm(x, y, gain, eps, dtype):
+    """(r, n, codes, scales): n = r gain / sqrt(mean(r^2) + eps), a row of zeros zeros for any eps."""
+    with np.errstate(all="ignore"):
+        r = x if y is None else R.to_type(x + y, dtype)
+        p = r if gain is None else r * gain
+        rms = np.sqrt((r * r).mean(-1) + float(np.float32(eps)))
+        n = np.where(rms[:, None] == 0, p, p / rms[:, None])    # p is 0 there, or 0 times a gain that is not finite
+        fine = np.isfinite(r).all(-1)
+        c, s = R.codes(np.where(fine[:, None], p, np.nan), np.where(rms == 0, 0.0, 1 / rms))
+    return r, n, c, s
+
+
+def check_norm(x, y, gain, eps, tag):
+    res, out = torch.full_like(x, 3.0), torch.full_like(x, 3.0)
+    q = prox.rmsnorm_q8(x, y, gain, eps, residual=res, out=out)
+    r, n, c, s = norm(f64(x), None if y is None else f64(y), None if gain is None else f64(gain), eps, x.dtype)
+    assert np.array_equal(f64(res), r, equal_nan=True), f"{tag}: residual"
+    R.check_codes(q.codes, c, tag)
+    R.check_scales(q.scales, s, tag)
+    R.check_out(out, n, x.dtype, tag)
+    alone = prox.rmsnorm(x, y, gain, eps)
+    assert torch.equal(alone.view(torch.int16), out.view(torch.int16)), tag
+    return out
+
+
+# One for every way in which a row is cut among threads.
+WIDTHS = [8, 96, 511, 512, 1500, 4000, 8192, 9000, 20000, 40001]
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_norm_of_rows_that_are_not_finite(d, dtype, eps):
+    x, y, gain = randn((9, d), 1, dtype), randn((9, d), 2, dtype), randn((d,), 3, dtype)
+    nan, inf, big = float("nan"), float("inf"), torch.finfo(dtype).max
+    x[1, 5], y[2, d - 1], x[3, 0], x[4, 7], y[4, 7] = nan, nan, inf, inf, -inf
+    x[5, 3], y[5, 3] = big, big              # the residual overflows
+    x[6], y[6] = 0, 0
+    x[7], y[7] = nan, nan
+    for g in (gain, None):
+        out = check_norm(x, y, g, eps, f"{d}")
+        # A NaN spoils its row; behind an infinite one the others are 0, and it is NaN.
+        assert torch.isnan(out[[1, 2, 4, 7]]).all() and (out[6] == 0).all()
+        assert torch.isnan(out[3, 0]) and torch.isnan(out[5, 3]) and (out[3, 1:] == 0).all() and (out[5, 4:] == 0).all()
+        assert torch.isfinite(out[[0, 8]]).all()
+    check_norm(x, None, gain, eps, f"{d}, nothing added")
+    gain[2] = inf
+    check_norm(x, y, gain, eps, f"{d}, gain")
+    gain[2] = nan
+    check_norm(x, y, gain, eps, f"{d}, gain NaN")
