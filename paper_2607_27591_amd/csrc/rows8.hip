@@ -121,12 +121,14 @@ __device__ __forceinline__ void both(double v, double &a, double &b) {
     a = __longlong_as_double((long long)(((uint64_t)h0 << 32) | l0));
     b = __longlong_as_double((long long)(((uint64_t)h1 << 32) | l1));
 }
+// f symmetric: the same bits in every lane, since every step joins pairs of lanes that see each other.  A rotation by 4
+// of 16 lanes does so once lanes 8 apart agree, so after that by 8 (before it, sums in 64 bits differ between quads).
 template <typename V, typename F>
-__device__ __forceinline__ V wave_join(V v, F f) {   // f symmetric: the same bits in every lane
+__device__ __forceinline__ V wave_join(V v, F f) {
     v = f(v, peer<1>(v));
     v = f(v, peer<2>(v));
-    v = f(v, peer<4>(v));
     v = f(v, peer<8>(v));
+    v = f(v, peer<4>(v));
     V a, b;
     both<16>(v, a, b);
     v = f(a, b);

@@ -65,3 +65,18 @@ def test_norm_of_rows_that_are_not_finite(d, dtype, eps):
     check_norm(x, y, gain, eps, f"{d}, gain")
     gain[2] = nan
     check_norm(x, y, gain, eps, f"{d}, gain NaN")
+
+
+@pytest.mark.parametrize("swap", [False, True])
+def test_lanes_of_a_row_agree_on_its_mean(swap):
+    # A row of one wave whose 64-bit sum of squares, 2^119 and little more, goes to one of two neighbours by the order in which
+    # its lanes' parts are added: the quads of lanes that hold 4 and 2 squares of 2^62 each lose them, or not.  The mean is then at
+    # 2^110 or above, where the kernel turns to 64 bits: lanes that take different ways do not see each other's largest.
+    r = torch.zeros((4, 4, 4, 8))                    # rows of 16 lanes, quads of 4, elements of a lane
+    r[:, int(swap)::2, :, :2] = 2.0 ** 56            # every quad's squares: 2^115
+    r[:, 1 - int(swap)::2, :2, :1] = 2.0 ** 57
+    r[:, 0, :, 4] = 2.0 ** 31
+    r[:, 3, :2, 4] = 2.0 ** 31
+    x = r.reshape(1, 512).to(BF16).cuda()
+    check_norm(x.expand(5, 512).contiguous(), None, None, 0.0, "rows")
+    check_norm(x.expand(5, 512).contiguous(), None, torch.linspace(1, 2, 512).to(BF16).cuda(), 0.0, "gain")
