@@ -475,8 +475,9 @@ __global__ __launch_bounds__(C::threads) void gated_kernel(QuantArgs A) {
     low = __uint_as_float(lows | 0x80000000u);
     const float topf = __uint_as_float(top);
     bool slow = !(topf >= 0x1p-60f && topf <= 0x1p100f);   // ends of the range, not finite
+    const float rel_top = rel_act<ACT>(fmaxf(low, kFarGate<ACT>));   // topf is off by this much, unless a far gate makes the largest
     if (!slow) {
-        const float s = 127.0f / topf, rel_top = rel_act<ACT>(fmaxf(low, kFarGate<ACT>)), from = topf * (1.0f - 0x1p-14f);
+        const float s = 127.0f / topf, from = topf * (1.0f - 0x1p-14f);
         each<CH>([&](auto c) {
             const int i = (c * T + t) * 8, n = d - i;
             if (n <= 0) return;
@@ -511,7 +512,7 @@ __global__ __launch_bounds__(C::threads) void gated_kernel(QuantArgs A) {
         return row_join<T, true>(most, parts, Most());
     };
     uint32_t most = largest();
-    if (!slow && __uint_as_float(most) > topf * (1.0f + 0x1p-13f)) {   // a gate below kFarGate made it: the codes are not near
+    if (!slow && fabsf(__uint_as_float(most) - topf) > rel_top * topf) {   // a far gate makes it: the codes may be off by more
         slow = true;
         most = largest();
     }

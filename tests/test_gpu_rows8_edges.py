@@ -80,3 +80,48 @@ def test_lanes_of_a_row_agree_on_its_mean(swap):
     x = r.reshape(1, 512).to(BF16).cuda()
     check_norm(x.expand(5, 512).contiguous(), None, None, 0.0, "rows")
     check_norm(x.expand(5, 512).contiguous(), None, torch.linspace(1, 2, 512).to(BF16).cuda(), 0.0, "gain")
+
+
+def just_above(act, far):
+    """(g, u, far u): an activation of the gate `far` that is larger than that of g by 5e-5 to 1.1e-4 of it."""
+    us = (1 + np.arange(128) / 128) * 2.0 ** 127
+    tops = R.act(np.full(128, far), us, act)
+    gates = f64((2 + torch.arange(512) / 512).to(BF16))
+    gates = np.unique(gates)
+    scale = 2.0 ** np.floor(np.log2(np.abs(tops).max()))
+    ups = (1 + np.arange(128) / 128) * scale / 4
+    v = R.act(gates[:, None], ups[None, :], act)
+    ratio = np.abs(tops)[:, None, None] / v[None]
+    a, b, c = np.argwhere((ratio > 1 + 5e-5) & (ratio < 1 + 1.1e-4))[0]
+    return gates[b], ups[c], us[a], v[b, c]
+
+
+@pytest.mark.parametrize("far", [-88.5, -90.0])
+@pytest.mark.parametrize("d", [100, 3000, 9000, 20000])
+def test_a_silu_gate_that_32_bits_lose_makes_the_largest(d, far):
+    check_far(prox.SILU, d, far)
+
+
+@pytest.mark.parametrize("far", [-13.375, -13.5])
+@pytest.mark.parametrize("d", [100, 3000, 9000, 20000])
+def test_a_gelu_gate_that_32_bits_lose_makes_the_largest(d, far):
+    check_far(prox.GELU, d, far)
+
+
+def check_far(act, d, far):
+    # By so little that the codes are all but those of the largest of the others, and only those near a border differ.
+    g0, u0, u1, top = just_above(act, far)
+    g, u = randn((5, d), 1, BF16), randn((5, d), 2, BF16)
+    size = np.abs(R.act(f64(g), f64(u), act)).max()
+    u = (u.float() * (0.9 * top / size)).to(BF16)
+    u[3:] = (torch.linspace(0.2, 0.99, d) * u0).to(BF16).cuda()      # rows of codes that are far from 0
+    g[3:] = float(g0)
+    g[:, d // 3], u[:, d // 3] = float(g0), float(u0)
+    g[:, d // 2], u[:, d // 2] = far, float(u1)
+    x, up = f64(g), f64(u)
+    v = np.abs(R.act(x, up, act))
+    assert (v.argmax(-1) == d // 2).all() and (v[:, d // 2] < 1.00012 * np.sort(v, -1)[:, -2]).all()
+    q = prox.quant_q8(g, u, act)
+    c, s = R.codes(R.act(x, up, act))
+    R.check_codes(q.codes, c, f"{d}")
+    R.check_scales(q.scales, s, f"{d}")
