@@ -266,8 +266,9 @@ __global__ __launch_bounds__(C::threads) void rmsnorm_kernel(NormArgs A) {
     row_join2<T>(sum, sums, Add(), top, tops, Most());
     const double mean = fma(sum, A.inv_d, (double)A.eps);
     const float topf = __uint_as_float(top);
-    // Products and 1 / rms well inside 32 bits, everything finite.
-    if (topf >= 0x1p-60f && topf <= 0x1p100f && mean >= 0x1p-110 && mean <= 0x1p110) {
+    // Products and 1 / rms well inside 32 bits, everything finite.  Products below 2^-126 lose bits: 2^-150, which a 1 / rms of
+    // 2^12 at most (any with eps from 6e-8) leaves far below the smallest step of the dtype.
+    if (topf >= 0x1p-60f && topf <= 0x1p100f && mean >= 0x1p-24 && mean <= 0x1p110) {
         // 1 / sqrt(mean) to about 2^-50: 32 bits, and two terms of the series of what is left.
         const double y0 = (double)__builtin_amdgcn_rsqf((float)mean), left = fma(-mean * y0, y0, 1.0);
         const double inv = fma(y0 * left, fma(left, 0.375, 0.5), y0);
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(C::threads) void rmsnorm_kernel(NormArgs A) {
             if (n <= 0) return;
             float p[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = elem<DT>(r[c], e) * elem<DT>(g[c], e);   // exact: 22 bits at most
+            for (int e = 0; e < 8; ++e) p[e] = elem<DT>(r[c], e) * elem<DT>(g[c], e);   // 22 bits at most: exact from 2^-126 on
             if (A.out) {
                 const uint4 w = make_uint4(round_pair<DT>(p[0] * invf, p[1] * invf), round_pair<DT>(p[2] * invf, p[3] * invf),
                                            round_pair<DT>(p[4] * invf, p[5] * invf), round_pair<DT>(p[6] * invf, p[7] * invf));

@@ -82,6 +82,18 @@ def test_lanes_of_a_row_agree_on_its_mean(swap):
     check_norm(x.expand(5, 512).contiguous(), None, torch.linspace(1, 2, 512).to(BF16).cuda(), 0.0, "gain")
 
 
+@pytest.mark.parametrize("d", [64, 500, 1000, 3000, 9000])
+def test_norm_of_small_products(d):
+    # Products r gain below 32 bits' normal range, and a 1 / rms that brings them back into it: eps 0 and a row of 2^-40 to 2^-49.
+    gen = torch.Generator().manual_seed(d)
+    for small in (40, 45, 49):
+        x = torch.randn((6, d), generator=gen) * 2.0 ** -105
+        x[:, d // 2] = 2.0 ** -small * (1 + torch.arange(6) / 8)
+        gain = 2.0 ** -torch.randint(20, 46, (d,), generator=gen).float() * (1 + torch.rand(d, generator=gen))
+        gain[d // 2] = 2.0 ** -9
+        check_norm(x.to(BF16).cuda(), None, gain.to(BF16).cuda(), 0.0, f"{d}, {small}")
+
+
 def just_above(act, far):
     """(g, u, far u): an activation of the gate `far` that is larger than that of g by 5e-5 to 1.1e-4 of it."""
     us = (1 + np.arange(128) / 128) * 2.0 ** 127
