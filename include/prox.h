@@ -640,7 +640,8 @@ prox_status prox_pack_linear_w8(const void *w, const prox_w8_linear *q, hipStrea
 /* Inverse view, for inspection and tests: codes int8 [n][k] and scales fp32 [n], device. */
 prox_status prox_unpack_linear_w8(const prox_w8_linear *q, int8_t *codes, float *scales, hipStream_t stream);
 
-/* The projection of rows in 8 bits (d = k; ldc <= PROX_MAX_Q8_PITCH).  codes may hold any int8.
+/* The projection of rows in 8 bits (d = k; ldc <= PROX_MAX_Q8_PITCH).  codes may hold any int8.  Rows
+ * and outputs make fewer than 2^23 blocks of 256 x 256 (2^22 rows: 130816 outputs; 2^20 outputs: 524032 rows).
  *   bias  device [n] (2-byte aligned), or NULL
  *   y     device, row b at y + b * ldy, 2-byte aligned; ldy >= n (ignored for one row)
  * One or two launches, no workspace.  A row's result does not depend on the other rows, nor on

@@ -271,7 +271,7 @@ prox_status prox_linear_w8(const prox_w8_linear *q, const int8_t *codes, int64_t
     if (!codes_ok(codes, ldc, scales, rows, q->k) || !y || !aligned(y, 2) || !aligned(bias, 2)) return PROX_ERR_INVALID;
     if (rows > 1 && ldy < q->n) return PROX_ERR_INVALID;
     if (rows > 1 && ldc > PROX_MAX_Q8_PITCH) return PROX_ERR_UNSUPPORTED;   // offsets inside a tile of rows: 32 bits
-    if (((long long)rows + 15) / 16 * ((q->n + 255) / 256) > kMaxGrid) return PROX_ERR_UNSUPPORTED;
+    if (!linear_w8_fits(rows, q->n)) return PROX_ERR_UNSUPPORTED;
     const Linear8Layout L(q->n, q->k);
     const auto *blob = static_cast<const uint8_t *>(q->blob);
     const Linear8Args a{blob, reinterpret_cast<const float *>(blob + L.scales), q->n, q->k, L.kblocks, codes, scales, rows > 1 ? ldc : 0, rows,

@@ -374,11 +374,17 @@ struct W8Cost {
     float start, few, all;   // us; per 1024 inputs with one workgroup under way, and 256
 };
 constexpr int kW8Variants = 12;
+constexpr long long kW8MaxGrid = 1 << 23;
 constexpr W8Cost kW8Cost[kW8Variants] = {{256, 256, 5.0f, 8.4f, 12.6f}, {128, 256, 4.0f, 4.7f, 7.0f}, {128, 128, 4.0f, 2.7f, 4.2f},
                                          {64, 256, 3.5f, 3.0f, 5.0f},   {64, 128, 3.0f, 1.6f, 2.6f},  {32, 128, 2.5f, 1.2f, 1.8f},
                                          {64, 64, 3.0f, 1.1f, 1.6f},    {32, 64, 2.4f, 0.7f, 1.05f},  {32, 32, 1.8f, 0.35f, 0.5f},
                                          {16, 64, 1.5f, 0.6f, 0.85f},   {16, 32, 1.3f, 0.3f, 0.45f},  {16, 16, 1.0f, 0.25f, 0.35f}};
 constexpr float kW8Launch = 2.0f;
+
+// Workgroups of 512 threads, within the 32 bits of a grid.
+inline bool w8_fits(const W8Cost &c, int rows, int n) {
+    return ((long long)rows + c.rows - 1) / c.rows * ((n + c.outs - 1) / c.outs) < kW8MaxGrid;
+}
 
 inline float w8_time(const W8Cost &c, int rows, int n, float k1024) {
     const long long tiles = ((long long)rows + c.rows - 1) / c.rows * ((n + c.outs - 1) / c.outs), full = tiles / 256;
@@ -388,11 +394,12 @@ inline float w8_time(const W8Cost &c, int rows, int n, float k1024) {
     return t;
 }
 
-inline int w8_variant(int rows, int n, float k1024, float *least) {
+inline int w8_variant(int rows, int n, float k1024, float *least) {   // the largest tiles fit (linear_w8_fits)
     int best = 0;
-    for (int v = 0; v < kW8Variants; ++v) {
+    *least = w8_time(kW8Cost[0], rows, n, k1024);
+    for (int v = 1; v < kW8Variants; ++v) {
         const float t = w8_time(kW8Cost[v], rows, n, k1024);
-        if (v == 0 || t < *least) best = v, *least = t;
+        if (t < *least && w8_fits(kW8Cost[v], rows, n)) best = v, *least = t;
     }
     return best;
 }
@@ -427,7 +434,7 @@ hipError_t launch_dt(const Linear8Args &a, hipStream_t s) {
         const W8Cost &c = kW8Cost[v];
         const long long mtiles = ((long long)a.rows + c.rows - 1) / c.rows, ntiles = (a.n + c.outs - 1) / c.outs;
         const long long whole = mtiles * ntiles / 256 * 256 / mtiles;   // columns of tiles of the whole rounds
-        if (whole < 1 || whole >= ntiles) continue;
+        if (whole < 1 || whole >= ntiles || !w8_fits(c, a.rows, a.n)) continue;
         const int n0 = (int)whole * c.outs;
         float t;
         const int u = w8_variant(a.rows, a.n - n0, k1024, &t);
@@ -446,6 +453,8 @@ hipError_t launch_dt(const Linear8Args &a, hipStream_t s) {
     if (b.bias) b.bias += cut;
     return run_variant<DT>(rest, b, s);
 }
+
+bool linear_w8_fits(int rows, int n) { return w8_fits(kW8Cost[0], rows, n); }
 
 hipError_t launch_linear_w8(int dtype, const Linear8Args &a, hipStream_t s) {
     return dtype == kBF16 ? launch_dt<kBF16>(a, s) : launch_dt<kF16>(a, s);

@@ -19,6 +19,7 @@ struct Linear8Args {
 };
 hipError_t launch_pack_linear_w8(int dtype, const void *w, int n, int k, void *blob, hipStream_t s);
 hipError_t launch_unpack_linear_w8(const void *blob, int n, int k, int8_t *codes, float *scales, hipStream_t s);
+bool linear_w8_fits(int rows, int n);   // its tiles, the largest at the least, in one grid
 hipError_t launch_linear_w8(int dtype, const Linear8Args &a, hipStream_t s);
 
 }  // namespace prox
