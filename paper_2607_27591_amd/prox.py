@@ -698,7 +698,7 @@ def linear_w4(q: LinearW4, x: torch.Tensor, bias: Optional[torch.Tensor] = None,
         if bias.numel() != q.n:
             raise ValueError("bias must be [n]")
     _same_device(dev, q.blob, y, bias)
-    _check(_on(dev, lib().prox_linear_w4, q.pointer(), x.data_ptr(), ldx, batch, _at(bias), y.data_ptr(), ldy),
+    _check(_on(dev, lib().prox_linear_w4, q.pointer(), x.data_ptr(), ldx, _int32(batch), _at(bias), y.data_ptr(), ldy),
            "prox_linear_w4")
     return y
 

@@ -14,6 +14,17 @@ def randn(shape, seed, dtype, scale=1.0):
     return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * scale).to(dtype).cuda()
 
 
+def test_linear_w4_refuses_batches_past_32_bits():
+    """They do not lose their upper bits: one row is not taken for all."""
+    w = prox.pack_linear_w4(randn((32, 128), 1, BF16))
+    x, y = randn((1, 128), 2, BF16), torch.zeros((1, 32), dtype=BF16, device="cuda")
+    for rows in (2 ** 32 + 1, 2 ** 32 + 2, 2 ** 31):
+        with pytest.raises(prox.ProxError) as e:
+            prox.linear_w4(w, x.expand(rows, 128), y=y.expand(rows, 32))
+        assert e.value.status == 1
+    assert (y == 0).all()
+
+
 def test_linear_w8_of_the_most_rows():
     # 2^22 rows of 8200 outputs: y of 69 GB.
     rows, n, k, few = prox.MAX_Q8_ROWS, 8200, 16, 4096
