@@ -195,12 +195,9 @@ __device__ __forceinline__ v4f mfma32(uint4 a, uint4 b, v4f c) {
 }
 
 // D += A B of 8-bit integers with 32-bit accumulation, exact.  16 x 16 x 64: lane l holds A[l % 16][16 (l / 16) + e]
-// and B[16 (l / 16) + e][l % 16], e = 0..15, and gets D[4 (l / 16) + e][l % 16].  32 x 32 x 32: A[l % 32][16 (l / 32)
-// + e], B alike, D[8 (e / 4) + 4 (l / 32) + e % 4][l % 32], e = 0..15.
+// and B[16 (l / 16) + e][l % 16], e = 0..15, and gets D[4 (l / 16) + e][l % 16].
 typedef int v4i __attribute__((ext_vector_type(4)));
-typedef int v16i __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ v4i mfma16_i8(v4i a, v4i b, v4i c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ v16i mfma32_i8(v4i a, v4i b, v16i c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
 
 // A word of 8 codes (n = q + 8, in the order of nibble_of) as an operand of mfma32: exact
 // 16-bit values under an exponent, 8 and 7 instructions.  The low half of a register holds

@@ -261,7 +261,7 @@ struct LinearLayout {
 // ---------------------------------------------------------------------------
 // codes   [block of 64 outputs][block of 64 inputs, an even number][tile 0..3][lane 0..63][16]: lane l of tile t
 //         holds inputs 16 (l / 16) .. + 15 of the output w8_output(t, l % 16) of the block: its operand of a
-//         16 x 16 x 64 MFMA (or, with its pair's, of 32 x 32 x 32), and a wave's load one run of 1024 bytes.
+//         16 x 16 x 64 MFMA, and a wave's load one run of 1024 bytes.
 //         0 past n and k.
 // scales  (256-aligned) fp32 [output], 0 past n.
 // The outputs of a tile are spread so that a lane, which gets rows 4 h + e of each tile's result, has 16

@@ -268,6 +268,8 @@ __global__ __launch_bounds__(C::threads) void rmsnorm_kernel(NormArgs A) {
     const float topf = __uint_as_float(top);
     // Products and 1 / rms well inside 32 bits, everything finite.  Products below 2^-126 lose bits: 2^-150, which a 1 / rms of
     // 2^12 at most (any with eps from 6e-8) leaves far below the smallest step of the dtype.
+    // Rows of a smaller rms go the 64-bit way (2048 x 8192 of rms 1e-5, eps 0: 47 us, else 21); a power of 2 of 1 / rms multiplied in
+    // first keeps them here, but takes 1 to 3% of every call with a 16-bit output.
     if (topf >= 0x1p-60f && topf <= 0x1p100f && mean >= 0x1p-24 && mean <= 0x1p110) {
         // 1 / sqrt(mean) to about 2^-50: 32 bits, and two terms of the series of what is left.
         const double y0 = (double)__builtin_amdgcn_rsqf((float)mean), left = fma(-mean * y0, y0, 1.0);
