@@ -8,9 +8,9 @@ CPU only; not collected by pytest.  Run ``python tests/host_sanitizers.py``.
 2. ``libprox.so`` is built with the host code of ``api.hip`` and
    ``api_layer.hip`` (the argument checks and dispatch) instrumented the same
    way by hipcc. The device code and the other sources are built as usual.
-   ``test_api_cpu.py``, ``test_api_layer_cpu.py`` and ``test_layer_ints_cpu.py``,
-   which call every entry point with invalid arguments and never reach a HIP
-   call, then run with clang's sanitizer runtime preloaded.
+   The tests of ``API_TESTS``, which call every entry point with invalid
+   arguments and never reach a HIP call, then run with clang's sanitizer runtime
+   preloaded.
 
 Leak detection is off: the interpreter's own allocations are not ours.
 Exits non-zero on the first sanitizer report or test failure.
@@ -30,7 +30,8 @@ from paper_2607_27591_amd import build as B   # noqa: E402  (compiler flags and 
 ORACLE_TESTS = ["test_oracle_pins.py", "test_oracle_geglu.py", "test_oracle_threshold.py",
                 "test_oracle_w4.py", "test_cost_model.py", "test_calibrate_cpu.py"]
 API_SOURCES = ["api.hip", "api_layer.hip"]
-API_TESTS = ["test_api_cpu.py", "test_api_layer_cpu.py", "test_layer_ints_cpu.py"]
+API_TESTS = ["test_api_cpu.py", "test_api_layer_cpu.py", "test_layer_ints_cpu.py", "test_rows8_cpu.py",
+             "test_linear_limits_cpu.py"]
 ENV = {"ASAN_OPTIONS": "detect_leaks=0:abort_on_error=0:halt_on_error=1",
        "UBSAN_OPTIONS": "halt_on_error=1:print_stacktrace=1"}
 
