@@ -2,7 +2,7 @@
 // the product: y^T = W x^T as 16 x 16 x 64 MFMAs, exact in 32 bits.  The weights go from the caches to registers as
 // operands (every wave's outputs are its own, and their layout is the operands'), x through LDS, where the waves share it;
 // the sums are scaled and rounded once.  Few rows are bound by the weights' bytes (28672 x 8192, 16 rows 40.1 us,
-// 5.9 TB/s), many by power: at 4096 rows the clock falls to 1.85 GHz (697 to 711 us, 2710 to 2760 TOP/s).  What saves power there:
+// 5.9 TB/s), many by power: at 4096 rows the clock falls to 1.85 GHz (693 to 731 us by the card, 2630 to 2780 TOP/s).  What saves power there:
 // 16 x 16 x 64 products rather than 32 x 32 x 32 (random operands, nothing else: 3695 and 3160 TOP/s), one operand
 // kept from product to product (4075 TOP/s).
 #include "linear_w8.hpp"
@@ -362,6 +362,7 @@ hipError_t launch_unpack_linear_w8(const void *blob, int n, int k, int8_t *codes
 
 // The variant by shape: the one that takes least by a model of its rounds of 256 workgroups, one a CU: each its start
 // and last step, and a time per 1024 inputs that grows with the workgroups under way, as they share the L2s and the power.
+// The weights' bytes from HBM, which all variants read alike for few rows, are left out: it ranks, and is no estimate there.
 // Larger tiles read less for each product, which bounds all but the largest; smaller ones fill the CUs.  In us at
 // k = 4096 (bf16, streams of calls), for 1 round and for 4:
 //   256 x 256  59.8, 227    128 x 256  34.2, 142    128 x 128  22.0, 84    64 x 256  21.7, 96    64 x 128  14.2, 53

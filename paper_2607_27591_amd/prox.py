@@ -1019,7 +1019,7 @@ def rmsnorm_q8(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: Optional
 
 
 def quant_q8(x: torch.Tensor, up: Optional[torch.Tensor] = None, act: int = SILU, q: Optional[RowsQ8] = None) -> RowsQ8:
-    """Rows in 8 bits: of x, or of act(x) * up (SILU or GELU)."""
+    """Rows in 8 bits: of act(x) * up (SILU or GELU), or, without up, of x itself (act plays no part)."""
     r = _Rows16(x)
     ldu, pu = (0, None) if up is None else (r.like(up, "up"), up.data_ptr())
     if q is None:
